@@ -536,13 +536,93 @@ int w4a4_dequant_epilogue(const int32_t *acc, const w4a4_act *A, const w4a4_weig
                           const w4a4_epilogue *ep, void *out, float *out_scale, float *out_zero,
                           int32_t *out_gsum, void *stream);
 
+/* ---- token generation -----------------------------------------------------------------------
+ * A decoder that writes one token at a time reads its weights and the keys and values of the tokens before, and computes
+ * little.  Its linears take the 4-bit weights of this library with 16-bit activations (the activations of a few tokens are not
+ * worth quantizing: W is what is read); keys and values are kept in 8 bits, in blocks that a block table names. */
+typedef enum { W4A4_F16 = 0, W4A4_BF16 = 1 } w4a4_dtype;
+
+/* out[M,N] = act(X[M,K] * deq(W)^T + bias[N]); X, bias and out in `dtype`, sums in fp32, no rounding in between.
+ * X [M, ldx] (ldx elements, a multiple of 8), W canonical codes of either mode, one scale per channel or per group of a multiple
+ * of 32 codes (rowsum_deq and esum are not read), bias may be NULL, out dense; pointers 16-byte aligned.  Meant for up to 64
+ * tokens (W is read once for every 64).  act: w4a4_act_fn, GELU on the fp32 value. */
+int w4a4_linear_w4a16(const void *X, int dtype, int M, int K, int ldx, const w4a4_weight *W, const void *bias, int act,
+                      void *out, void *stream);
+
+/* One step's bookkeeping of the blocks of a cache, entirely on the device.
+ *   lens[r]        tokens of request r in the cache; new_tokens[r]: tokens that it adds in this step, negative: it has ended
+ *   table          [requests, width] blocks of each request in order; entries behind its last block mean nothing
+ *   ring, state    ring of `capacity` block numbers: state[1] free ones from place state[0] on
+ * A request takes the blocks that its new tokens need from the ring, in the order of requests; one whose need (with that of all
+ * requests before it) passes the free blocks takes none, nor does one whose tokens would pass width * block: it is not
+ * served.  The blocks of an ended request go back behind the free ones.  A request with a length that is no length
+ * (negative, or past width * block) is left alone.
+ *   lens_out[r]    lens[r] + new_tokens[r] where served, 0 where ended, else lens[r];  state_out[2]: the state afterwards
+ *   start          [requests + 1] sums of the new tokens: request r's are tokens start[r] .. start[r+1]-1 of the step
+ *   slots, positions  [tokens] of each new token, in that order: block * (tokens of a block) + place in it, and its place in its
+ *                  request; -1 for tokens of requests that are not served and behind the last one.  Tokens past `tokens` are left out.
+ * table and ring are updated in place (entries that change); state_out and lens_out are other arrays than state and lens, which
+ * makes the call repeatable.  block: 16, 32, 64 or 128 tokens.  ring must hold at most `capacity` free blocks in all. */
+int w4a4_kv8_plan(const int32_t *lens, const int32_t *new_tokens, int requests, int32_t *table, int width, int32_t *ring,
+                  int capacity, const int32_t *state, int block, int tokens, int32_t *state_out, int32_t *lens_out,
+                  int32_t *start, int32_t *slots, int32_t *positions, void *stream);
+
+/* The cache of one layer: int8 codes, one scale (>= 0) for each block and head.  Value = code * scale. */
+typedef struct {
+    int8_t *k;              /* [blocks, heads, block, features]                                */
+    int8_t *v;              /* [blocks, heads, features, block]: a feature's tokens lie together */
+    float  *k_scale;        /* [blocks, heads]                                                 */
+    float  *v_scale;
+    int blocks, heads;
+    int block;              /* tokens of a block: 16, 32, 64 or 128                            */
+    int features;           /* of a head: 64, 96, 128 or 256                                   */
+} w4a4_kv8_cache;
+
+/* Writes new keys and values into their slots (block * (tokens of a block) + place; what is no slot of the cache, -1 for instance,
+ * is skipped).  K, V: [tokens, heads * features] in `dtype`, rows ldk and ldv elements apart (multiples of 8).
+ * The tokens of one block stand together in `slots`, in any order, and no slot comes twice: w4a4_kv8_plan leaves them so (if not, what that block
+ * holds afterwards is unspecified).  A block that gets its first slot begins anew: what it held is lost, its scale is the new tokens'
+ * largest magnitude / 127.  Otherwise the scale is raised where the new tokens need it, and the codes that stay are scaled
+ * down by old / new, to nearest even.  Codes are x * (1 / scale), to nearest even, at most 127 in magnitude; an infinity becomes +-127 and a NaN 0, and neither
+ * counts for the scale. A scale below the smallest normal number is stored as 0. */
+int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv,
+                    const int32_t *slots, void *stream);
+
+/* Keys and values of `tokens` slots, K and V [tokens, heads, features] in `dtype`; zeros for what is no slot. */
+int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream);
+
+/* The queries of an attention call. */
+typedef struct {
+    const void    *q;       /* [tokens, ldq]: the first heads * features elements of a row     */
+    const int32_t *table;   /* [requests, width] blocks of each request                        */
+    const int32_t *lens;    /* [requests] keys of each request, its new tokens among them      */
+    const int32_t *start;   /* [requests + 1]: queries start[r] .. start[r+1]-1 are request r's */
+    float scale;            /* of the scores, > 0                                              */
+    int dtype;              /* w4a4_dtype of q and of the output                               */
+    int tokens, heads;      /* heads: a multiple of the cache's (grouped heads)                */
+    int ldq;                /* elements, a multiple of 8                                       */
+    int requests, width;
+    int queries, context;   /* upper bounds of a request's queries and keys                    */
+    int window;             /* keys that a query sees, itself included; 0: all before it       */
+} w4a4_kv8_queries;
+
+/* out [tokens, heads, features], lse [tokens, heads] (may be NULL): causal attention of each request's queries, its last positions,
+ * over its keys in the cache, and the logarithm of the sum of exp(score).  A query that sees nothing (a request of no
+ * keys, a row that pads the batch) gets zeros and -infinity.  Rows of tokens that belong to no request are not written.
+ * `queries` must hold (queries beyond it are not computed); keys past `context` only cost time.  A table entry that names no block
+ * of the cache hides its keys.  The workspace (16-byte aligned) is free again when the call's work has finished. */
+size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q);
+int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void *out, float *lse, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* A call of one of the entry points with its arguments laid out once, for callers to whom passing a dozen of them costs as
  * much as the launch (through Python's ctypes 1.5 us and more, of this 0.3).  p, i, f and n hold the entry point's pointers,
  * ints, float and size in the order of its parameters, the stream excepted; structs that a pointer names must still be there when
  * the call is made.  Returns what the entry point returns, W4A4_ERR_INVALID_ARG for another `entry`. */
 typedef enum {
     W4A4_CALL_QUANTIZE_ACT = 0, W4A4_CALL_LINEAR = 1, W4A4_CALL_LINEAR_F16ACT = 2, W4A4_CALL_LAYERNORM_QUANTIZE = 3,
-    W4A4_CALL_QUANTIZE_ROWS8 = 4, W4A4_CALL_LINEAR8 = 5        /* w8a8_quantize_rows, w8a8_linear */
+    W4A4_CALL_QUANTIZE_ROWS8 = 4, W4A4_CALL_LINEAR8 = 5,       /* w8a8_quantize_rows, w8a8_linear */
+    W4A4_CALL_LINEAR_W4A16 = 6, W4A4_CALL_KV8_PLAN = 7, W4A4_CALL_KV8_APPEND = 8, W4A4_CALL_KV8_READ = 9, W4A4_CALL_KV8_ATTENTION = 10
 } w4a4_call_entry;
 typedef struct {
     void *p[10];

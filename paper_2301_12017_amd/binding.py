@@ -75,6 +75,18 @@ class _Call(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p * 10), ("n", ctypes.c_size_t), ("i", ctypes.c_int * 6), ("f", ctypes.c_float), ("entry", ctypes.c_int)]
 
 
+class _KV8Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("blocks", ctypes.c_int), ("heads", ctypes.c_int), ("block", ctypes.c_int), ("features", ctypes.c_int)]
+
+
+class _KV8Queries(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("dtype", ctypes.c_int), ("tokens", ctypes.c_int), ("heads", ctypes.c_int),
+                ("ldq", ctypes.c_int), ("requests", ctypes.c_int), ("width", ctypes.c_int), ("queries", ctypes.c_int),
+                ("context", ctypes.c_int), ("window", ctypes.c_int)]
+
+
 class _LayerWeights(ctypes.Structure):
     _fields_ = [("hidden", ctypes.c_int), ("heads", ctypes.c_int), ("ffn", ctypes.c_int),
                 ("qkv", _Part), ("attn_out", _Part), ("ffn1", _Part), ("ffn2", _Part),
@@ -128,6 +140,12 @@ _SIGNATURES = {
     "w4a4_probe_stream": (_i, [_vp, _vp, _sz, _vp, _vp]),
     "w4a4_pick_schedule": (_i, [ctypes.POINTER(_Act), ctypes.POINTER(_Weight), ctypes.POINTER(_Epilogue)]),
     "w4a4_gemm_i32": (_i, [ctypes.POINTER(_Act), ctypes.POINTER(_Weight), _vp, _i, _vp]),
+    "w4a4_linear_w4a16": (_i, [_vp, _i, _i, _i, _i, ctypes.POINTER(_Weight), _vp, _i, _vp, _vp]),
+    "w4a4_kv8_plan": (_i, [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "w4a4_kv8_append": (_i, [ctypes.POINTER(_KV8Cache), _vp, _vp, _i, _i, _i, _i, _vp, _vp]),
+    "w4a4_kv8_read": (_i, [ctypes.POINTER(_KV8Cache), _vp, _i, _i, _vp, _vp, _vp]),
+    "w4a4_kv8_attention_workspace_bytes": (_sz, [ctypes.POINTER(_KV8Cache), ctypes.POINTER(_KV8Queries)]),
+    "w4a4_kv8_attention": (_i, [ctypes.POINTER(_KV8Cache), ctypes.POINTER(_KV8Queries), _vp, _vp, _vp, _sz, _vp]),
     "w4a4_run_call": (_i, [ctypes.POINTER(_Call), _vp]),
     "w4a4_dequant_epilogue": (_i, [_vp, ctypes.POINTER(_Act), ctypes.POINTER(_Weight),
                                    ctypes.POINTER(_Epilogue), _vp, _vp, _vp, _vp, _vp]),
@@ -425,7 +443,8 @@ class _Prepared:
     """A call of an entry point with its arguments laid out once (w4a4_call in include/w4a4.h): calling the object only makes the C
     call on the current stream.  Handing the dozen arguments to the entry point itself took 1.5 us of the 3.8 that such a call
     cost on the host, more than the kernels of few tokens leave to hide it behind."""
-    ENTRIES = ("w4a4_quantize_act", "w4a4_linear", "w4a4_linear_f16act", "w4a4_layernorm_quantize", "w8a8_quantize_rows", "w8a8_linear")
+    ENTRIES = ("w4a4_quantize_act", "w4a4_linear", "w4a4_linear_f16act", "w4a4_layernorm_quantize", "w8a8_quantize_rows", "w8a8_linear",
+               "w4a4_linear_w4a16", "w4a4_kv8_plan", "w4a4_kv8_append", "w4a4_kv8_read", "w4a4_kv8_attention")
 
     def _lay_out(self, name, pointers, ints=(), f=0.0, n=0):
         self.name = name
@@ -790,6 +809,164 @@ class PreparedQuantizeAct(_Prepared):
         M, K = X.shape
         self._lay_out("w4a4_quantize_act", (X, out.q, out.scale, out.zero, out.gsum, out.osum),
                       (M, K, X.stride(0), out.mode, out.group, out.layout))
+
+
+# ---- token generation --------------------------------------------------------------------------------
+F16, BF16 = 0, 1
+_DTYPES = {torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    assert t in _DTYPES, f"{t}: fp16 or bf16"
+    return _DTYPES[t]
+
+
+def _i32(*tensors):
+    for t in tensors:
+        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+
+
+class PreparedLinearW4A16(_Prepared):
+    """A w4a4_linear_w4a16 call: 16-bit activations X [M, K] (fp16 or bf16, rows may be strided) of a few tokens times 4-bit
+    weights in canonical codes.  The result, in the type of X, is in `out`."""
+
+    def __init__(self, X: torch.Tensor, W: QWeight, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None):
+        assert X.is_cuda and X.dim() == 2 and X.stride(1) == 1
+        assert bias is None or (bias.dtype == X.dtype and bias.shape == (W.N,) and bias.is_contiguous())
+        M, K = X.shape
+        if out is None:
+            out = torch.empty((M, W.N), dtype=X.dtype, device=X.device)
+        assert out.dtype == X.dtype and out.shape == (M, W.N) and out.is_contiguous()
+        self.out, self.w = out, W.c()
+        self.keep = (X, W, bias)
+        self._lay_out("w4a4_linear_w4a16", (X, self.w, bias, out), (_dtype(X.dtype), M, K, X.stride(0) if M > 1 else max(K, X.stride(0)), act))
+
+
+def linear_w4a16(X: torch.Tensor, W: QWeight, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """w4a4_linear_w4a16: [M, N] in the type of X."""
+    call = PreparedLinearW4A16(X, W, bias, act, out)
+    call()
+    return call.out
+
+
+class KVCache8:
+    """The 8-bit cache of one layer (w4a4_kv8_cache in include/w4a4.h): codes k [blocks, heads, block, features] and
+    v [blocks, heads, features, block], scales [blocks, heads]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        self.blocks, self.heads, self.block, self.features = k.shape
+        assert v.shape == (self.blocks, self.heads, self.features, self.block) and k_scale.shape == v_scale.shape == (self.blocks, self.heads)
+        assert k.dtype == v.dtype == torch.int8 and k_scale.dtype == v_scale.dtype == torch.float32
+        assert all(t.is_cuda and t.is_contiguous() for t in (k, v, k_scale, v_scale))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    @classmethod
+    def new(cls, blocks: int, heads: int, features: int, block=16, device="cuda"):
+        """An empty cache: its codes and scales are zeros."""
+        codes = lambda *shape: torch.zeros(shape, dtype=torch.int8, device=device)
+        return cls(codes(blocks, heads, block, features), codes(blocks, heads, features, block),
+                   *(torch.zeros((blocks, heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+    def c(self) -> _KV8Cache:
+        return _KV8Cache(_address(self.k), _address(self.v), _address(self.k_scale), _address(self.v_scale), self.blocks, self.heads, self.block, self.features)
+
+
+class PreparedKV8Plan(_Prepared):
+    """A w4a4_kv8_plan call: the block bookkeeping of a step for at most `tokens` new tokens.  table and ring are updated in place; the
+    results are in `state`, `lens`, `start`, `slots` and `positions`.  A loop over steps lets the calls take turns: one with
+    the outputs of the other as its lens and state (lens_out, state_out)."""
+
+    def __init__(self, lens, new_tokens, table, ring, state, block: int, tokens: int, lens_out=None, state_out=None):
+        _i32(lens, new_tokens, table, ring, state)
+        R, dev = lens.numel(), lens.device
+        assert new_tokens.numel() == R and table.dim() == 2 and table.shape[0] == R and state.numel() == 2
+        new = lambda n: torch.empty((n,), dtype=torch.int32, device=dev)
+        self.lens, self.state = new(R) if lens_out is None else lens_out, new(2) if state_out is None else state_out
+        _i32(self.lens, self.state)
+        assert self.lens.numel() == R and self.state.numel() == 2
+        self.start, self.slots, self.positions = new(R + 1), new(tokens), new(tokens)
+        self.table, self.ring = table, ring
+        self.keep = (lens, new_tokens, state)
+        self._lay_out("w4a4_kv8_plan", (lens, new_tokens, table, ring, state, self.state, self.lens, self.start, self.slots, self.positions),
+                      (R, table.shape[1], ring.numel(), block, tokens))
+
+
+def kv8_plan(lens, new_tokens, table, ring, state, block: int, tokens: int) -> PreparedKV8Plan:
+    """w4a4_kv8_plan, once: the call, with its results."""
+    call = PreparedKV8Plan(lens, new_tokens, table, ring, state, block, tokens)
+    call()
+    return call
+
+
+def _kv_rows(C: KVCache8, x: torch.Tensor) -> int:
+    """Elements between the rows of x [tokens, heads, features]; the heads of a token lie together."""
+    assert x.is_cuda and x.dim() == 3 and x.shape[1:] == (C.heads, C.features) and x.stride(2) == 1
+    assert C.heads == 1 or x.stride(1) == C.features
+    return max(x.stride(0), C.heads * C.features) if x.shape[0] <= 1 else x.stride(0)
+
+
+class PreparedKV8Append(_Prepared):
+    """A w4a4_kv8_append call: K and V [tokens, heads, features] (slices of a fused projection as they are) into their slots."""
+
+    def __init__(self, cache: KVCache8, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor):
+        _i32(slots)
+        T = K.shape[0]
+        assert K.dtype == V.dtype and V.shape == K.shape and slots.numel() >= T
+        self.keep, self.c = (cache, K, V, slots), cache.c()
+        self._lay_out("w4a4_kv8_append", (self.c, K, V, slots), (_dtype(K.dtype), T, _kv_rows(cache, K), _kv_rows(cache, V)))
+
+
+def kv8_append(cache: KVCache8, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor):
+    PreparedKV8Append(cache, K, V, slots)()
+
+
+class PreparedKV8Read(_Prepared):
+    """A w4a4_kv8_read call: keys and values of `slots`, in `k` and `v` [tokens, heads, features]."""
+
+    def __init__(self, cache: KVCache8, slots: torch.Tensor, dtype=torch.float16):
+        _i32(slots)
+        T = slots.numel()
+        self.k, self.v = (torch.empty((T, cache.heads, cache.features), dtype=dtype, device=slots.device) for _ in range(2))
+        self.keep, self.c = (cache, slots), cache.c()
+        self._lay_out("w4a4_kv8_read", (self.c, slots, self.k, self.v), (T, _dtype(dtype)))
+
+
+def kv8_read(cache: KVCache8, slots: torch.Tensor, dtype=torch.float16):
+    call = PreparedKV8Read(cache, slots, dtype)
+    call()
+    return call.k, call.v
+
+
+class PreparedKV8Attention(_Prepared):
+    """A w4a4_kv8_attention call: queries q [tokens, heads, features] over the cache.  `queries` and `context` are upper bounds of a
+    request's queries and keys.  The results are in `out` and, where asked for, `lse`."""
+
+    def __init__(self, q: torch.Tensor, cache: KVCache8, table: torch.Tensor, lens: torch.Tensor, start: torch.Tensor, queries: int, context: int,
+                 scale: float, window=0, want_lse=False, out: Optional[torch.Tensor] = None):
+        _i32(table, lens, start)
+        T, G, D = q.shape
+        R = lens.numel()
+        assert q.is_cuda and D == cache.features and q.stride(2) == 1 and (G == 1 or q.stride(1) == D)
+        assert table.dim() == 2 and table.shape[0] == R and start.numel() == R + 1
+        ldq = max(q.stride(0), G * D) if T <= 1 else q.stride(0)
+        if out is None:
+            out = torch.empty((T, G, D), dtype=q.dtype, device=q.device)
+        assert out.dtype == q.dtype and out.shape == (T, G, D) and out.is_contiguous()
+        self.out, self.lse = out, torch.empty((T, G), dtype=torch.float32, device=q.device) if want_lse else None
+        self.c = cache.c()
+        self.q = _KV8Queries(_address(q), _address(table), _address(lens), _address(start), scale, _dtype(q.dtype), T, G, ldq, R, table.shape[1],
+                             queries, context, window)
+        need = int(lib().w4a4_kv8_attention_workspace_bytes(ctypes.byref(self.c), ctypes.byref(self.q)))
+        self.workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+        self.keep = (q, cache, table, lens, start)
+        self._lay_out("w4a4_kv8_attention", (self.c, self.q, self.out, self.lse, self.workspace), n=need)
+
+
+def kv8_attention(q, cache, table, lens, start, queries: int, context: int, scale: float, window=0, want_lse=False):
+    """w4a4_kv8_attention: out [tokens, heads, features], or (out, lse)."""
+    call = PreparedKV8Attention(q, cache, table, lens, start, queries, context, scale, window, want_lse)
+    call()
+    return (call.out, call.lse) if want_lse else call.out
 
 
 def gemm_i32(A: QAct, W: QWeight, schedule=0) -> torch.Tensor:

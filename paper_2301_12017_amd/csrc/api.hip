@@ -37,6 +37,7 @@ extern "C" int w4a4_run_call(const w4a4_call *c, void *st) {
     auto i32 = [&](int k) { return static_cast<int32_t *>(p[k]); };
     auto f32 = [&](int k) { return static_cast<float *>(p[k]); };
     auto ep = [&](int k) { return static_cast<const w4a4_epilogue *>(p[k]); };
+    auto cache = [&](int k) { return static_cast<const w4a4_kv8_cache *>(p[k]); };
     auto weight = [&](int k) { return static_cast<const w4a4_weight *>(p[k]); };
     switch (c->entry) {
         case W4A4_CALL_QUANTIZE_ACT:
@@ -51,6 +52,16 @@ extern "C" int w4a4_run_call(const w4a4_call *c, void *st) {
             return w8a8_quantize_rows(p[0], i[0], i[1], i[2], i8(1), f32(2), st);
         case W4A4_CALL_LINEAR8:
             return w8a8_linear(i8(0), i[0], f32(1), i[1], i8(2), f32(3), i[2], i[3], ep(4), p[5], st);
+        case W4A4_CALL_LINEAR_W4A16:
+            return w4a4_linear_w4a16(p[0], i[0], i[1], i[2], i[3], weight(1), p[2], i[4], p[3], st);
+        case W4A4_CALL_KV8_PLAN:
+            return w4a4_kv8_plan(i32(0), i32(1), i[0], i32(2), i[1], i32(3), i[2], i32(4), i[3], i[4], i32(5), i32(6), i32(7), i32(8), i32(9), st);
+        case W4A4_CALL_KV8_APPEND:
+            return w4a4_kv8_append(cache(0), p[1], p[2], i[0], i[1], i[2], i[3], i32(3), st);
+        case W4A4_CALL_KV8_READ:
+            return w4a4_kv8_read(cache(0), i32(1), i[0], i[1], p[2], p[3], st);
+        case W4A4_CALL_KV8_ATTENTION:
+            return w4a4_kv8_attention(cache(0), static_cast<const w4a4_kv8_queries *>(p[1]), p[2], f32(3), p[4], c->n, st);
         default: return W4A4_ERR_INVALID_ARG;
     }
 }
