@@ -957,7 +957,7 @@ class PreparedKV8Attention(_Prepared):
         self.q = _KV8Queries(_address(q), _address(table), _address(lens), _address(start), scale, _dtype(q.dtype), T, G, ldq, R, table.shape[1],
                              queries, context, window)
         need = int(lib().w4a4_kv8_attention_workspace_bytes(ctypes.byref(self.c), ctypes.byref(self.q)))
-        self.workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+        self.workspace = torch.zeros((need,), dtype=torch.uint8, device=q.device) if need else None
         self.keep = (q, cache, table, lens, start)
         self._lay_out("w4a4_kv8_attention", (self.c, self.q, self.out, self.lse, self.workspace), n=need)
 

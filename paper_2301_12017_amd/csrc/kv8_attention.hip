@@ -19,8 +19,10 @@
 // each, of the size of the output's own rounding) with v_scale in them; they are held at c * v_scale, c a power of two per
 // wave that keeps the largest product near 2^13, so that weights down to 2^-27 keep all their bits.
 //
-// Bound by the bytes of the cache for single tokens: keys are shared out over pieces (workgroups) and the waves of each; pieces
-// leave their sum, maximum and unfinished output in the workspace, and a second kernel joins them in a fixed order.
+// Bound by the bytes of the cache for single tokens.  A (request, tile of rows, key head) is a group; a workgroup takes a group or,
+// where requests are long, a piece of one: every workgroup finds from the lengths by itself how long a piece is and
+// which one is its own.  The pieces of a group leave sum, maximum and unfinished output in the workspace, and the one that
+// comes last joins them, in their order (a counter says who that is, not in which order sums are taken).
 #include "gen.hpp"
 
 namespace w4a4 {
@@ -29,8 +31,19 @@ int kv8_cache_check(const w4a4_kv8_cache *C);
 
 namespace {
 
-constexpr int kWaves = 4, kStep = 64;                              // waves of a workgroup, keys of a step
+constexpr int kStep = 64;                                          // keys of a step
+constexpr int kSlots = 512, kMostGroups = 4096;                    // pieces of few groups, and groups that are cut, at most
+constexpr int kCounters = kSlots + kMostGroups;                    // in the workspace
 constexpr float kUnset = 1.2676506e30f;                            // 2^100: c before a scale of values has been seen
+
+// n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).
+struct Div {
+    uint64_t by;
+    int d;
+    explicit Div(int d) : by(((1ull << 32) + d - 1) / d), d(d) {}
+    __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * by) >> 32); }
+    __device__ __forceinline__ int rest(int n, int q) const { return n - q * d; }
+};
 
 struct AttnArgs {
     const uint16_t *q;
@@ -38,35 +51,35 @@ struct AttnArgs {
     const float *k_scale, *v_scale;
     const int32_t *table, *lens, *start;
     uint16_t *out;
-    float *lse, *po, *pml;                                         // joined later: [row][piece][D], [row][piece][2]
+    float *lse, *po, *pml;                                         // pieces of groups: [workgroup][row][D] and [..][row][2]
+    int *arrived;
     long ldq;
-    int tokens, blocks, H, group, shift, width, window, queries, pieces, piece;
+    int tokens, blocks, H, shift, width, window, queries, requests, slots;
+    Div group, tiles, heads;                                       // queries of a head of the cache; tiles of a request; = H
     float scale;                                                   // in powers of two: scale / ln 2
 };
 
-// The rows of one workgroup and the keys they see.
+// The rows of a group and the keys they see.
 struct Tile {
     int first, n, len, rows, row0;                                 // first token, queries, keys of the request; rows of it; this tile's first
     int begin, end;                                                // keys that any row of the tile sees
+    int steps;                                                     // 0: no rows; else one at least
 };
 __device__ __forceinline__ Tile tile_of(const AttnArgs &a, int r, int row0, int tile) {
     Tile t;
     t.first = max(a.start[r], 0);
     t.n = min(min(a.start[r + 1], a.tokens) - t.first, a.queries);
-    t.rows = t.n > 0 ? t.n * a.group : 0;
+    t.rows = t.n > 0 ? t.n * a.group.d : 0;
     t.len = min(max(a.lens[r], 0), (int)min((long)a.width << a.shift, 0x7fffff00L));
     t.row0 = row0;
-    t.begin = t.end = 0;
+    t.begin = t.end = t.steps = 0;
     if (row0 < t.rows) {
-        const int lo = t.len - t.n + row0 / a.group, hi = t.len - t.n + (min(row0 + tile, t.rows) - 1) / a.group;
+        const int lo = t.len - t.n + a.group.of(row0), hi = t.len - t.n + a.group.of(min(row0 + tile, t.rows) - 1);
         t.end = max(hi + 1, 0);
         t.begin = a.window ? min(max(lo - a.window + 1, 0), t.end) : 0;
+        t.steps = t.end > t.begin ? (t.end - (t.begin & ~(kStep - 1)) + kStep - 1) / kStep : 1;
     }
     return t;
-}
-__device__ __forceinline__ int pieces_of(const AttnArgs &a, const Tile &t) {   // pieces begin at a whole step
-    const int keys = t.end - (t.begin & ~(kStep - 1));
-    return t.end > t.begin ? min((keys + a.piece - 1) / a.piece, a.pieces) : 0;
 }
 
 template <typename Op>
@@ -78,6 +91,18 @@ __device__ __forceinline__ float over_groups(float x, Op op) {     // op over th
 }
 __device__ __forceinline__ float max2(float x, float y) { return fmaxf(x, y); }
 __device__ __forceinline__ float add2(float x, float y) { return x + y; }
+
+// Two floats at the coherence point, past the L2s (each XCD has its own): what workgroups leave for one another.  Release and
+// acquire fences at device scope would write back and invalidate a whole L2 each time (a call of 512 workgroups 208 us instead of 49).
+__device__ __forceinline__ void leave2(float *p, float x, float y) {
+    const unsigned long long v = __builtin_bit_cast(uint32_t, x) | (unsigned long long)__builtin_bit_cast(uint32_t, y) << 32;
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+struct Two { float x, y; };
+__device__ __forceinline__ Two take2(const float *p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return Two{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
+}
 
 // four codes of a word as four halves
 __device__ __forceinline__ u32x2_t codes4(uint32_t w) {
@@ -96,19 +121,95 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
 }
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // 2^e, -126 <= e <= 127
 
-// D features, NR tiles of sixteen rows.
-template <bool BF16, int D, int NR>
-__global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attention_kernel(AttnArgs a) {
+// s / t, rounded up, for s < 2^24 (a step more or less makes no difference to who uses it, but all use the same)
+__device__ __forceinline__ int pieces_in(int steps, int piece) { return (steps + piece - 1) / piece; }
+
+// How the groups are cut, and which piece is this workgroup's.  Each wave works it out by itself.
+struct Cut { int entry, head, piece, at; };                        // piece: steps of one; at: which one of the group (entry < 0: none)
+template <typename Entry>
+__device__ __forceinline__ Cut cut_of(const AttnArgs &a, int entries, int least, Entry entry) {
+    const int lane = threadIdx.x & 63, per = (entries + 63) / 64, e0 = min(lane * per, entries), e1 = min(e0 + per, entries);
+    auto plus = [](int x, int y) { return x + y; };
+    // equal shares of all steps, and larger pieces until there are no more of them than places for workgroups (where groups are
+    // more than the places, a piece more for each place)
+    int mine = 0, only = 0;
+    for (int i = e0; i < e1; ++i) mine += only = entry(i).steps;
+    const float fair = (float)lanes_reduce<64>(mine, plus) * (float)a.H / (float)a.slots;
+    const int most = entries * a.H <= a.slots ? a.slots : entries * a.H + a.slots;
+    constexpr float kMore[8] = {1.0f, 1.1f, 1.25f, 1.4f, 1.6f, 2.0f, 2.5f, 3.5f};
+    int piece = 0x1000000, count[8] = {};
+    auto size = [&](int j) { return max((int)__builtin_ceilf(fair * kMore[j]), least); };
+    for (int i = e0; i < e1; ++i) {
+        const int steps = per == 1 ? only : entry(i).steps;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) count[j] += pieces_in(steps, size(j));
+    }
+#pragma unroll
+    for (int j = 7; j >= 0; --j)
+        if (lanes_reduce<64>(count[j], plus) * a.H <= most) piece = size(j);
+    mine = 0;
+    for (int i = e0; i < e1; ++i) mine += pieces_in(per == 1 ? only : entry(i).steps, piece);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += u;
+    }
+    const unsigned long long in = __ballot((int)blockIdx.x < upto * a.H);
+    Cut c{-1, 0, piece, 0};
+    if (!in) return c;
+    const int owner = __builtin_ctzll(in);
+    int before = __builtin_amdgcn_readlane(upto - mine, owner), e = min(owner * per, entries - 1);
+    for (;; ++e) {                                                 // (one round where a lane has one entry)
+        const int n = per == 1 ? __builtin_amdgcn_readlane(mine, owner) : pieces_in(entry(e).steps, piece);
+        if ((int)blockIdx.x < (before + n) * a.H || e + 1 >= entries) break;
+        before += n;
+    }
+    const int in_entry = blockIdx.x - before * a.H;
+    c.entry = e;
+    c.at = a.heads.of(in_entry);                                   // (the heads of a request side by side: they read neighbouring memory)
+    c.head = a.heads.rest(in_entry, c.at);
+    return c;
+}
+
+// D features, NR tiles of sixteen rows, NW waves.  CUT: groups may be cut; else a workgroup per group.
+template <bool BF16, int D, int NR, int NW, bool CUT>
+__global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kernel(AttnArgs a) {
     constexpr int NT = D / 16, KW = D / 64, KT = D % 64 != 0;      // feature tiles; 64-feature loads of a key, and one of 32
-    extern __shared__ __attribute__((aligned(16))) float smem[];   // [wave][NR * NT * 4][64], then m, l and c of [wave][NR * 16]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, kg = lane >> 4;
-    const int r = blockIdx.z, h = blockIdx.y % a.H, tile = blockIdx.y / a.H, p = blockIdx.x;
-    const Tile t = tile_of(a, r, tile * 16 * NR, 16 * NR);
-    if (t.row0 >= t.rows) return;
-    const int np = pieces_of(a, t);
-    if (p >= max(np, 1)) return;
-    const int base = (t.begin & ~(kStep - 1)) + p * a.piece, stop = p + 1 >= a.pieces ? t.end : min(base + a.piece, t.end);
-    const int steps = stop > base ? (stop - base + kStep - 1) / kStep : 0;
+    constexpr int ROWS = NR * 16, REGS = NR * NT * 4, PART = NW * ROWS;
+    constexpr bool AHEAD = D * NR <= 128 || D == 256;              // keys AND values of the next step are fetched during this one
+    extern __shared__ __attribute__((aligned(16))) float smem[];   // [wave][REGS][64], then m, l and 1 / c of [wave][ROWS]
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int entries = a.requests * a.tiles.d;
+    auto entry = [&](int e) {
+        const int r = a.tiles.of(e);
+        return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
+    };
+    Cut cut;
+    if constexpr (CUT) {
+        cut = cut_of(a, entries, NW, entry);
+        if (cut.entry < 0) return;
+    } else {
+        cut.entry = a.heads.of(blockIdx.x);
+        cut.head = a.heads.rest(blockIdx.x, cut.entry);
+        cut.piece = cut.at = 0;
+    }
+    const int r = a.tiles.of(cut.entry), h = cut.head;
+    const int lane = tid & 63, col = lane & 15, kg = lane >> 4, kgroup = col >> 2;
+    // Blocks of the lane's rows of K and of its lane group's keys.  What lies behind a request's last block may be anything, but
+    // the row of the table is there: the first ones are asked for before the request's length is known.
+    struct Ids { int k, v; };
+    const int32_t *ids_of = a.table + (size_t)r * a.width;
+    auto fetch_ids = [&](int key0) { return Ids{ids_of[min((key0 + 16 * kgroup) >> a.shift, a.width - 1)], ids_of[min((key0 + 16 * kg) >> a.shift, a.width - 1)]}; };
+    const int first_step = cut.at * cut.piece;
+    Ids next = {0, 0};
+    if (a.width && !a.window) next = fetch_ids((first_step + wave) * kStep);
+    const Tile t = entry(cut.entry);
+    if (!t.steps) return;
+    const int np = CUT ? pieces_in(t.steps, cut.piece) : 1, steps = CUT ? min(cut.piece, t.steps - first_step) : t.steps;
+    const int base = (t.begin & ~(kStep - 1)) + first_step * kStep, stop = min(base + steps * kStep, t.end);
+    const int todo = stop > base ? steps : 0;
+    if (a.window && wave < todo) next = fetch_ids(base + wave * kStep);
 
     // the lane's rows
     int hi[NR], lo[NR];                                            // last and first key that each sees
@@ -116,10 +217,10 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
     float back[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-        const int row = min(t.row0 + 16 * i + col, t.rows - 1), j = row / a.group;
+        const int row = min(t.row0 + 16 * i + col, t.rows - 1), j = a.group.of(row);
         hi[i] = t.len - t.n + j;
         lo[i] = a.window ? hi[i] - a.window + 1 : 0;
-        const uint16_t *src = a.q + (long)(t.first + j) * a.ldq + (h * a.group + row % a.group) * D;
+        const uint16_t *src = a.q + (long)(t.first + j) * a.ldq + (h * a.group.d + a.group.rest(row, j)) * D;
 #pragma unroll
         for (int c = 0; c < KW; ++c)
 #pragma unroll
@@ -142,26 +243,23 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
                 q[i][c][w] = pack_halves(to_float<BF16>((uint16_t)q[i][c][w]) * up, to_float<BF16>((uint16_t)(q[i][c][w] >> 16)) * up);
     }
     // wave-uniform: keys that all rows of the tile see
-    const int all_hi = t.len - t.n + t.row0 / a.group;
-    const int all_lo = a.window ? t.len - t.n + (min(t.row0 + 16 * NR, t.rows) - 1) / a.group - a.window + 1 : 0;
+    const int all_hi = t.len - t.n + a.group.of(t.row0);
+    const int all_lo = a.window ? t.len - t.n + a.group.of(min(t.row0 + 16 * NR, t.rows) - 1) - a.window + 1 : 0;
 
-    struct Ids { int k, v; bool ok; };                             // blocks of the lane's rows of K and of its lane group's keys
-    const int32_t *ids_of = a.table + (size_t)r * a.width;
-    const int kgroup = col >> 2, mask = (1 << a.shift) - 1;
-    auto fetch_ids = [&](int s) {
-        const int key0 = base + kStep * s, kk = key0 + 16 * kgroup, kv = key0 + 16 * kg;
-        Ids d;
-        d.k = kk < stop && kk + 15 >= t.begin ? ids_of[kk >> a.shift] : -1;
-        d.v = kv < stop && kv + 15 >= t.begin ? ids_of[kv >> a.shift] : -1;
-        d.ok = (unsigned)d.v < (unsigned)a.blocks;
-        if ((unsigned)d.k >= (unsigned)a.blocks) d.k = 0;
-        if (!d.ok) d.v = 0;
-        return d;
+    const int mask = (1 << a.shift) - 1;
+    struct Blocks { int k, v; bool ok; };                          // ok: the lane group's keys are there
+    auto settle = [&](const Ids &d, int s) {
+        const int kv = base + kStep * s + 16 * kg;
+        Blocks b;
+        b.ok = (kv < stop) & (kv + 15 >= t.begin) & ((unsigned)d.v < (unsigned)a.blocks);
+        b.k = (unsigned)d.k < (unsigned)a.blocks ? d.k : 0;
+        b.v = (unsigned)d.v < (unsigned)a.blocks ? d.v : 0;
+        return b;
     };
     u32x4_t kw[4][KW], vw[NT];
     u32x2_t kt[4];
     float ks, vs, ksn = 0, vsn = 0;
-    auto fetch_k = [&](const Ids &d, int s) {
+    auto fetch_k = [&](const Blocks &d, int s) {
         const int key = base + kStep * s + 16 * kgroup + (col & 3);
         const int8_t *src = a.k + ((((size_t)d.k * a.H + h) << a.shift) + (key & mask)) * D;
 #pragma unroll
@@ -171,10 +269,11 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
             if (KT) kt[T] = *reinterpret_cast<const u32x2_t *>(src + 4 * T * D + 64 * KW + 8 * kg);
         }
         const size_t unit = (size_t)d.v * a.H + h;
-        ksn = d.ok ? a.k_scale[unit] : 0.0f;
-        vsn = d.ok ? a.v_scale[unit] : 0.0f;
+        const float kx = a.k_scale[unit], vx = a.v_scale[unit];    // (of keys that are not there: whatever they hold)
+        ksn = d.ok ? kx : 0.0f;
+        vsn = d.ok ? vx : 0.0f;
     };
-    auto fetch_v = [&](const Ids &d, int s) {
+    auto fetch_v = [&](const Blocks &d, int s) {
         const int key = base + kStep * s + 16 * kg;
         const int8_t *src = a.v + ((((size_t)d.v * a.H + h) * D + col) << a.shift) + (key & mask);
 #pragma unroll
@@ -191,16 +290,16 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
         for (int n = 0; n < NT; ++n) o[i][n] = float4_t{0, 0, 0, 0};
     }
 
-    Ids now = {0, 0, false}, next = {0, 0, false};
-    if (wave < steps) {
-        now = fetch_ids(wave);
+    Blocks now = {0, 0, false}, then = now;                        // of this step, and of the wave's next
+    if (wave < todo) {
+        now = settle(next, wave);
         fetch_k(now, wave);
-        fetch_v(now, wave);
-        if (wave + kWaves < steps) next = fetch_ids(wave + kWaves);
+        if (AHEAD) fetch_v(now, wave);
+        if (wave + NW < todo) next = fetch_ids(base + (wave + NW) * kStep);
     }
-    for (int s = wave; s < steps; s += kWaves) {
+    for (int s = wave; s < todo; s += NW) {
         const int key0 = base + kStep * s;
-        const bool more = s + kWaves < steps, ok = now.ok;
+        const bool more = s + NW < todo, ok = now.ok;
         ks = ksn;
         vs = vsn;
         float4_t sc[NR][4];
@@ -222,7 +321,9 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
                 for (int i = 0; i < NR; ++i) sc[i][T] = mfma16<false>(x, q[i][2 * KW], sc[i][T]);
             }
         }
-        if (more) fetch_k(next, s + kWaves);
+        if (more) then = settle(next, s + NW);
+        if (AHEAD && more) fetch_k(then, s + NW);
+        if (!AHEAD) fetch_v(now, s);
 
         // c follows the scales of values
         if (__any(vs * c > 32768.0f)) {
@@ -251,9 +352,10 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
                 for (int e = 0; e < 4; ++e) x[4 * T + e] = sc[i][T][e] * kf;
             if (!plain) {
                 const int key = key0 + 16 * kg;                    // the lane's keys are key .. key + 15, in order
+                const int first = lo[i] - key;
+                const unsigned many = ok && hi[i] >= lo[i] ? hi[i] - lo[i] : 0, none = ok && hi[i] >= lo[i] ? 0 : 0x40000000;
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!ok || key + e > hi[i] || key + e < lo[i]) x[e] = -INFINITY;
+                for (int e = 0; e < 16; ++e) x[e] = (unsigned)(e - first) + none <= many ? x[e] : -INFINITY;
             }
             float mx = x[0];
 #pragma unroll
@@ -289,23 +391,22 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
                 for (int i = 0; i < NR; ++i) o[i][n] = mfma16<false>(x, pw[i][half], o[i][n]);
             }
         if (more) {
-            fetch_v(next, s + kWaves);
-            now = next;
-            if (s + 2 * kWaves < steps) next = fetch_ids(s + 2 * kWaves);
+            if (AHEAD) fetch_v(then, s + NW);
+            else fetch_k(then, s + NW);
+            now = then;
+            if (s + 2 * NW < todo) next = fetch_ids(base + (s + 2 * NW) * kStep);
         }
     }
 
     // the waves' parts of the same rows
-    constexpr int REGS = NR * NT * 4;
-    float *const ml = smem + kWaves * REGS * 64;                   // [m | l | 1 / c][wave][NR * 16]
-    constexpr int ROWS = NR * 16, PART = kWaves * ROWS;
+    float *const ml = smem + NW * REGS * 64;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const float sum = over_groups(l[i], add2);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) smem[(wave * REGS + (i * NT + n) * 4 + e) * 64 + lane] = o[i][n][e];
+            for (int f = 0; f < 4; ++f) smem[(wave * REGS + (i * NT + n) * 4 + f) * 64 + lane] = o[i][n][f];
         if (kg == 0) {
             ml[wave * ROWS + 16 * i + col] = m[i];
             ml[PART + wave * ROWS + 16 * i + col] = sum;
@@ -313,106 +414,172 @@ __global__ __launch_bounds__(kWaves * 64, D * NR >= 256 ? 1 : 2) void kv8_attent
         }
     }
     __syncthreads();
+    const bool whole = np <= 1;
+    for (int n = wave; n < NT; n += NW) {                          // sixteen features
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        const int row = t.row0 + 16 * i + col;
-        if (row >= t.rows) continue;
-        float mx = -INFINITY, sum = 0.0f, by[kWaves];
+        for (int i = 0; i < NR; ++i) {
+            const int row = t.row0 + 16 * i + col;
+            if (row >= t.rows) continue;
+            float mx = -INFINITY, sum = 0.0f, by[NW], y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, ml[w * ROWS + 16 * i + col]);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = ml[w * ROWS + 16 * i + col], e = mw > -INFINITY ? __builtin_amdgcn_exp2f(mw - mx) : 0.0f;
-            sum += e * ml[PART + w * ROWS + 16 * i + col];
-            by[w] = e * ml[2 * PART + w * ROWS + 16 * i + col];
-        }
-        const bool whole = np <= 1;
-        const float inv = whole ? (sum != 0.0f ? 1.0f / sum : 0.0f) : 1.0f;
-        const size_t at = (size_t)(t.first + row / a.group) * (a.H * a.group) + h * a.group + row % a.group;
-        for (int n = wave; n < NT; n += kWaves) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) y[e] += smem[(w * REGS + (i * NT + n) * 4 + e) * 64 + lane] * by[w];
-                y[e] *= inv;
+            for (int w = 0; w < NW; ++w) {
+                by[w] = ml[w * ROWS + 16 * i + col];
+                mx = fmaxf(mx, by[w]);
             }
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = by[w] > -INFINITY ? __builtin_amdgcn_exp2f(by[w] - mx) : 0.0f;
+                sum += f * ml[PART + w * ROWS + 16 * i + col];
+                by[w] = f * ml[2 * PART + w * ROWS + 16 * i + col];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] += smem[(w * REGS + (i * NT + n) * 4 + k) * 64 + lane] * by[w];
+            }
+            const int j = a.group.of(row);
+            const size_t at = ((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(row, j);
             if (whole) {
-                const uint32_t y0 = from_float<BF16>(y[0]) | (uint32_t)from_float<BF16>(y[1]) << 16;
-                const uint32_t y1 = from_float<BF16>(y[2]) | (uint32_t)from_float<BF16>(y[3]) << 16;
+                const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+                const uint32_t y0 = from_float<BF16>(y[0] * inv) | (uint32_t)from_float<BF16>(y[1] * inv) << 16;
+                const uint32_t y1 = from_float<BF16>(y[2] * inv) | (uint32_t)from_float<BF16>(y[3] * inv) << 16;
                 *reinterpret_cast<u32x2_t *>(a.out + at * D + 16 * n + 4 * kg) = u32x2_t{y0, y1};
+                if (n == 0 && kg == 0 && a.lse) a.lse[at] = sum != 0.0f ? (mx + log2f(sum)) * 0.69314718056f : -INFINITY;
             } else {
-                *reinterpret_cast<float4_t *>(a.po + (at * a.pieces + p) * D + 16 * n + 4 * kg) = float4_t{y[0], y[1], y[2], y[3]};
-            }
-        }
-        if (wave == 0 && kg == 0) {
-            if (!whole) {
-                a.pml[(at * a.pieces + p) * 2] = mx;
-                a.pml[(at * a.pieces + p) * 2 + 1] = sum;
-            } else if (a.lse) {
-                a.lse[at] = sum != 0.0f ? (mx + log2f(sum)) * 0.69314718056f : -INFINITY;
+                float *to = a.po + ((size_t)blockIdx.x * ROWS + 16 * i + col) * D + 16 * n + 4 * kg;
+                leave2(to, y[0], y[1]);
+                leave2(to + 2, y[2], y[3]);
+                if (n == 0 && kg == 0) leave2(a.pml + ((size_t)blockIdx.x * ROWS + 16 * i + col) * 2, mx, sum);
             }
         }
     }
-}
+    if (whole) return;
 
-// A wave per row: the pieces of a tile's rows.
-template <bool BF16, int D, int NR>
-__global__ __launch_bounds__(256) void kv8_join_kernel(AttnArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r = blockIdx.y, h = blockIdx.x % a.H, tile = blockIdx.x / a.H;
-    const Tile t = tile_of(a, r, tile * 16 * NR, 16 * NR);
-    if (t.row0 >= t.rows) return;
-    const int np = pieces_of(a, t);
-    if (np <= 1) return;
-    constexpr int F = (D + 63) / 64;
-    for (int row = t.row0 + wave; row < min(t.row0 + 16 * NR, t.rows); row += 4) {
-        const size_t at = (size_t)(t.first + row / a.group) * (a.H * a.group) + h * a.group + row % a.group;
-        const float *ml = a.pml + at * a.pieces * 2, *po = a.po + at * a.pieces * D;
-        float mx = -INFINITY, sum = 0.0f, y[F] = {};
-        for (int p = 0; p < np; ++p) mx = fmaxf(mx, ml[2 * p]);
-        for (int p = 0; p < np; ++p) {
-            const float e = ml[2 * p] > -INFINITY ? __builtin_amdgcn_exp2f(ml[2 * p] - mx) : 0.0f;
-            sum += e * ml[2 * p + 1];
-#pragma unroll
-            for (int f = 0; f < F; ++f)
-                if (64 * f + lane < D) y[f] += e * po[(size_t)p * D + 64 * f + lane];
+    // the pieces of the group are those of workgroups w0, w0 + H, ...
+    if constexpr (CUT) {
+    __shared__ int s_last;
+    const int w0 = blockIdx.x - cut.at * a.H;
+    __builtin_amdgcn_s_waitcnt(0);                                 // what this wave left is there before the workgroup's arrival is
+    __syncthreads();
+    if (tid == 0) {
+        s_last = __hip_atomic_fetch_add(a.arrived + w0, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == np - 1;
+        if (s_last) __hip_atomic_store(a.arrived + w0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
+    }
+    __syncthreads();
+    if (!s_last) return;
+    // maximum and sum of each row over the parts: THREADS / ROWS lanes a row
+    constexpr int THREADS = NW * 64, LANES = THREADS / ROWS, QUADS = D / 4;
+    const int rows = min(ROWS, t.rows - t.row0), parts = np;
+    auto part = [&](int w) { return (size_t)(w0 + w * a.H) * ROWS; };
+    {
+        const int row = tid / LANES;
+        float mx = -INFINITY, sum = 0.0f;
+        if (row < rows)
+            for (int w = tid % LANES; w < parts; w += LANES) {
+                const Two x = take2(a.pml + (part(w) + row) * 2);
+                if (x.x > -INFINITY) {
+                    const float to = fmaxf(mx, x.x);
+                    sum = sum * __builtin_amdgcn_exp2f(mx - to) + x.y * __builtin_amdgcn_exp2f(x.x - to);
+                    mx = to;
+                }
+            }
+        const float most = lanes_reduce<LANES>(mx, max2);
+        sum = lanes_reduce<LANES>(mx > -INFINITY ? sum * __builtin_amdgcn_exp2f(mx - most) : 0.0f, add2);
+        if (tid % LANES == 0) {
+            ml[row] = most;
+            ml[ROWS + row] = sum != 0.0f ? 1.0f / sum : 0.0f;
+            if (row < rows && a.lse) {
+                const int j = a.group.of(t.row0 + row);
+                a.lse[((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(t.row0 + row, j)] = sum != 0.0f ? (most + log2f(sum)) * 0.69314718056f : -INFINITY;
+            }
         }
-        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    }
+    __syncthreads();
+    // the outputs: four features of a row a thread; where rows are few, several threads share the parts
+    const int items = rows * QUADS, ways = max(THREADS / items, 1);
+    for (int i0 = 0; i0 < items; i0 += THREADS) {
+        const int i = ways > 1 ? tid % items : i0 + tid, way = ways > 1 ? tid / items : 0, row = i / QUADS, f = i % QUADS * 4;
+        const bool in = way < ways && i < items;
+        float4_t y = {0, 0, 0, 0};
+        if (in) {
+            const float most = ml[row];
+#pragma unroll 8
+            for (int w = way; w < parts; w += ways) {
+                const Two x = take2(a.pml + (part(w) + row) * 2), v0 = take2(a.po + (part(w) + row) * D + f), v1 = take2(a.po + (part(w) + row) * D + f + 2);
+                const float by = x.x > -INFINITY ? __builtin_amdgcn_exp2f(x.x - most) : 0.0f;
+                y[0] += by * v0.x;
+                y[1] += by * v0.y;
+                y[2] += by * v1.x;
+                y[3] += by * v1.y;
+            }
+        }
+        if (ways > 1) {
+            if (in) *reinterpret_cast<float4_t *>(smem + 4 * (way * items + i)) = y;
+            __syncthreads();
+            if (in && way == 0)
+                for (int k = 1; k < ways; ++k) {
+                    const float4_t v = *reinterpret_cast<const float4_t *>(smem + 4 * (k * items + i));
 #pragma unroll
-        for (int f = 0; f < F; ++f)
-            if (64 * f + lane < D) a.out[at * D + 64 * f + lane] = from_float<BF16>(y[f] * inv);
-        if (lane == 0 && a.lse) a.lse[at] = sum != 0.0f ? (mx + log2f(sum)) * 0.69314718056f : -INFINITY;
+                    for (int g = 0; g < 4; ++g) y[g] += v[g];
+                }
+        }
+        if (in && way == 0) {
+            const int j = a.group.of(t.row0 + row);
+            const float inv = ml[ROWS + row];
+            const size_t at = ((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(t.row0 + row, j);
+            const uint32_t y0 = from_float<BF16>(y[0] * inv) | (uint32_t)from_float<BF16>(y[1] * inv) << 16;
+            const uint32_t y1 = from_float<BF16>(y[2] * inv) | (uint32_t)from_float<BF16>(y[3] * inv) << 16;
+            *reinterpret_cast<u32x2_t *>(a.out + at * D + f) = u32x2_t{y0, y1};
+        }
+    }
     }
 }
 
-// How a call is shared out: tiles of rows, pieces of keys.
-struct Split { int nr, tiles, pieces, piece; };
+// How a call is shared out.
+struct Split {
+    int nr, tiles;
+    bool cut;                                                      // groups are cut where they are long
+    int places;                                                    // for pieces in the workspace
+};
 Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     Split s;
-    const int group = Q.heads / C.heads;
-    const long rows = (long)Q.queries * group;
-    s.nr = rows > 16 ? 2 : 1;
+    const long rows = (long)Q.queries * (Q.heads / C.heads);
+    s.nr = rows > 16 && C.features <= 128 ? 2 : 1;
     s.tiles = (int)((rows + 16 * s.nr - 1) / (16 * s.nr));
     const long keys = Q.window ? min((long)Q.context, (long)Q.window + 16 * s.nr + kStep) : Q.context;
-    const long groups = (long)s.tiles * C.heads * Q.requests;      // workgroups without pieces
-    long piece = (keys * groups + 1023) / 1024;
-    piece = (max(piece, 256L) + 255) / 256 * 256;
-    s.pieces = (int)max(1L, (keys + piece - 1) / piece);
-    s.piece = (int)piece;
+    const long groups = (long)s.tiles * C.heads * Q.requests;
+    // Finding the pieces and joining them costs 4 us, a round of eight steps of a group 2 us.  us whole | cut, 8 key heads of 128: one
+    // request of 1024 keys 11.2 | 13.0, 1280 12.6 | 13.0, 2048 16.4 | 13.0; eight of 1280 13.5 | 15.2, 2048 18.0 | 17.2; forty of 1280 30.5 | 29.3.
+    s.cut = keys > 20 * kStep && groups <= kMostGroups;
+    s.places = s.cut ? (int)groups + kSlots : 0;
     return s;
 }
 
-template <bool BF16, int D, int NR>
-int launch(AttnArgs &a, const Split &s, int requests, hipStream_t st) {
-    auto kern = kv8_attention_kernel<BF16, D, NR>;
-    constexpr size_t lds = ((size_t)kWaves * NR * (D / 16) * 4 * 64 + 3 * kWaves * NR * 16) * sizeof(float);
+template <bool BF16, int D, int NR, int NW, bool CUT>
+int launch_waves(AttnArgs &a, const Split &s, hipStream_t st) {
+    auto kern = kv8_attention_kernel<BF16, D, NR, NW, CUT>;
+    constexpr size_t lds = ((size_t)NW * NR * (D / 16) * 4 * 64 + 3 * NW * NR * 16) * sizeof(float);
     static KernelState ks;
-    if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
-    hipLaunchKernelGGL(kern, dim3(s.pieces, a.H * s.tiles, requests), dim3(kWaves * 64), lds, st, a);
-    if (s.pieces > 1) hipLaunchKernelGGL((kv8_join_kernel<BF16, D, NR>), dim3(a.H * s.tiles, requests), dim3(256), 0, st, a);
+    const void *fn = reinterpret_cast<const void *>(kern);
+    const int cus = prepare_kernel(fn, lds, ks);
+    if (cus < 0) return W4A4_ERR_HIP;
+    int grid = a.H * a.tiles.d * a.requests;
+    if (CUT) {
+        const int at_once = resident_per_cu(fn, NW * 64, lds, ks);
+        if (at_once <= 0) return W4A4_ERR_HIP;
+        a.slots = min(kSlots, cus * at_once);
+        grid = grid <= a.slots ? a.slots : grid + a.slots;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(NW * 64), lds, st, a);
     return launch_status();
+}
+
+template <bool BF16, int D, int NR>
+int launch(AttnArgs &a, const Split &s, hipStream_t st) {
+    constexpr int NW = D <= 128 ? 8 : 4;
+    if (!s.cut) return launch_waves<BF16, D, NR, NW, false>(a, s, st);
+    // Few groups: eight waves a workgroup, half as many pieces to join; more: four waves, two workgroups a CU, which hide each other's
+    // beginning and end.  us at 8 | 4 waves, 128 features: 8 groups of 150001 keys 63 | 68, 48 of 30000 and less 16.1 | 20.0; 256 groups, one request of 8000
+    // keys and 31 of 300, 51 | 18, 64 x 8 of 1280 45 | 36; 248 of 160 to 5000 keys 46 | 45.
+    if (a.H * a.tiles.d * a.requests <= 32) return launch_waves<BF16, D, NR, NW, true>(a, s, st);
+    return launch_waves<BF16, D, NR, 4, true>(a, s, st);
 }
 
 int check(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q) {
@@ -432,7 +599,7 @@ using namespace w4a4;
 extern "C" size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q) {
     if (check(C, Q) || !Q->tokens || !Q->requests || !Q->queries) return 0;
     const Split s = split_of(*C, *Q);
-    return s.pieces > 1 ? (size_t)Q->tokens * Q->heads * s.pieces * (C->features + 2) * sizeof(float) : 0;
+    return s.cut ? kCounters * sizeof(int) + (size_t)s.places * 16 * s.nr * (C->features + 2) * sizeof(float) : 0;
 }
 
 extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void *out, float *lse, void *workspace,
@@ -442,19 +609,25 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     if (!Q->q || !Q->lens || !Q->start || !out || (Q->width && !Q->table)) return W4A4_ERR_INVALID_ARG;
     if (!aligned16(Q->q) || !aligned16(out)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const Split s = split_of(*C, *Q);
-    if (Q->requests > 65535 || (long)C->heads * s.tiles > 65535) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    // steps are counted in 32 bits, and divisions (Div) are exact below 2^32
+    const int group = Q->heads / C->heads;
+    if (Q->requests > 65535 || (double)Q->queries * group * group > 4e9 || (double)Q->requests * s.tiles * max(s.tiles, C->heads * C->heads) > 4e9 ||
+        ((double)Q->width * C->block / kStep + 2) * C->heads * s.tiles * Q->requests > 2e9) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const size_t need = w4a4_kv8_attention_workspace_bytes(C, Q);
     if (need && (!workspace || workspace_bytes < need)) return W4A4_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    float *po = static_cast<float *>(workspace);
+    int *arrived = static_cast<int *>(workspace);
+    float *po = reinterpret_cast<float *>(arrived + (need ? kCounters : 0));
     AttnArgs a{static_cast<const uint16_t *>(Q->q), C->k, C->v, C->k_scale, C->v_scale, Q->table, Q->lens, Q->start,
-               static_cast<uint16_t *>(out), lse, po, po + (size_t)Q->tokens * Q->heads * s.pieces * C->features, Q->ldq, Q->tokens, C->blocks, C->heads,
-               Q->heads / C->heads, __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, s.pieces, s.piece, Q->scale * 1.44269504f};
+               static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
+               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
     auto run = [&](auto bf16, auto d) {
         constexpr bool BF = decltype(bf16)::value;
         constexpr int D = decltype(d)::value;
-        return s.nr == 2 ? launch<BF, D, 2>(a, s, Q->requests, st) : launch<BF, D, 1>(a, s, Q->requests, st);
+        if constexpr (D <= 128)
+            if (s.nr == 2) return launch<BF, D, 2>(a, s, st);
+        return launch<BF, D, 1>(a, s, st);
     };
     auto typed = [&](auto d) { return Q->dtype == W4A4_BF16 ? run(std::true_type{}, d) : run(std::false_type{}, d); };
     switch (C->features) {
