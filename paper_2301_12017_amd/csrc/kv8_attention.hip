@@ -23,74 +23,13 @@
 // where requests are long, a piece of one: every workgroup finds from the lengths by itself how long a piece is and
 // which one is its own.  The pieces of a group leave sum, maximum and unfinished output in the workspace, and the one that
 // comes last joins them, in their order (a counter says who that is, not in which order sums are taken).
-#include "gen.hpp"
+#include "kv8_attention.hpp"
 
 namespace w4a4 {
 
 int kv8_cache_check(const w4a4_kv8_cache *C);
 
 namespace {
-
-constexpr int kStep = 64;                                          // keys of a step
-constexpr int kSlots = 512, kMostGroups = 4096;                    // pieces of few groups, and groups that are cut, at most
-constexpr int kCounters = kSlots + kMostGroups;                    // in the workspace
-constexpr float kUnset = 1.2676506e30f;                            // 2^100: c before a scale of values has been seen
-
-// n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).
-struct Div {
-    uint64_t by;
-    int d;
-    explicit Div(int d) : by(((1ull << 32) + d - 1) / d), d(d) {}
-    __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * by) >> 32); }
-    __device__ __forceinline__ int rest(int n, int q) const { return n - q * d; }
-};
-
-struct AttnArgs {
-    const uint16_t *q;
-    const int8_t *k, *v;
-    const float *k_scale, *v_scale;
-    const int32_t *table, *lens, *start;
-    uint16_t *out;
-    float *lse, *po, *pml;                                         // pieces of groups: [workgroup][row][D] and [..][row][2]
-    int *arrived;
-    long ldq;
-    int tokens, blocks, H, shift, width, window, queries, requests, slots;
-    Div group, tiles, heads;                                       // queries of a head of the cache; tiles of a request; = H
-    float scale;                                                   // in powers of two: scale / ln 2
-};
-
-// The rows of a group and the keys they see.
-struct Tile {
-    int first, n, len, rows, row0;                                 // first token, queries, keys of the request; rows of it; this tile's first
-    int begin, end;                                                // keys that any row of the tile sees
-    int steps;                                                     // 0: no rows; else one at least
-};
-__device__ __forceinline__ Tile tile_of(const AttnArgs &a, int r, int row0, int tile) {
-    Tile t;
-    t.first = max(a.start[r], 0);
-    t.n = min(min(a.start[r + 1], a.tokens) - t.first, a.queries);
-    t.rows = t.n > 0 ? t.n * a.group.d : 0;
-    t.len = min(max(a.lens[r], 0), (int)min((long)a.width << a.shift, 0x7fffff00L));
-    t.row0 = row0;
-    t.begin = t.end = t.steps = 0;
-    if (row0 < t.rows) {
-        const int lo = t.len - t.n + a.group.of(row0), hi = t.len - t.n + a.group.of(min(row0 + tile, t.rows) - 1);
-        t.end = max(hi + 1, 0);
-        t.begin = a.window ? min(max(lo - a.window + 1, 0), t.end) : 0;
-        t.steps = t.end > t.begin ? (t.end - (t.begin & ~(kStep - 1)) + kStep - 1) / kStep : 1;
-    }
-    return t;
-}
-
-template <typename Op>
-__device__ __forceinline__ float over_groups(float x, Op op) {     // op over the lanes l % 16 + 16 g, in all of them
-    auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    x = op(__builtin_bit_cast(float, (unsigned)s[0]), __builtin_bit_cast(float, (unsigned)s[1]));
-    s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    return op(__builtin_bit_cast(float, (unsigned)s[0]), __builtin_bit_cast(float, (unsigned)s[1]));
-}
-__device__ __forceinline__ float max2(float x, float y) { return fmaxf(x, y); }
-__device__ __forceinline__ float add2(float x, float y) { return x + y; }
 
 // Two floats at the coherence point, past the L2s (each XCD has its own): what workgroups leave for one another.  Release and
 // acquire fences at device scope would write back and invalidate a whole L2 each time (a call of 512 workgroups 208 us instead of 49).
@@ -103,26 +42,6 @@ __device__ __forceinline__ Two take2(const float *p) {
     const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return Two{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
 }
-
-// four codes of a word as four halves
-__device__ __forceinline__ u32x2_t codes4(uint32_t w) {
-    w ^= 0x80808080u;
-    const half2_t off = {(_Float16)1152.0f, (_Float16)1152.0f};
-    const half2_t a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - off;
-    const half2_t b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - off;
-    return u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-}
-__device__ __forceinline__ u32x4_t codes8(uint32_t w0, uint32_t w1) {
-    const u32x2_t a = codes4(w0), b = codes4(w1);
-    return u32x4_t{a[0], a[1], b[0], b[1]};
-}
-__device__ __forceinline__ uint32_t pack_halves(float a, float b) {
-    return __builtin_bit_cast(uint32_t, half2_t{(_Float16)a, (_Float16)b});
-}
-__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // 2^e, -126 <= e <= 127
-
-// s / t, rounded up, for s < 2^24 (a step more or less makes no difference to who uses it, but all use the same)
-__device__ __forceinline__ int pieces_in(int steps, int piece) { return (steps + piece - 1) / piece; }
 
 // How the groups are cut, and which piece is this workgroup's.  Each wave works it out by itself.
 struct Cut { int entry, head, piece, at; };                        // piece: steps of one; at: which one of the group (entry < 0: none)
@@ -534,12 +453,13 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
 
 // How a call is shared out.
 struct Split {
-    int nr, tiles;
+    int nr, tiles;                                                 // nr: 0 for many rows (kv8_prompt.hip)
     bool cut;                                                      // groups are cut where they are long
     int places;                                                    // for pieces in the workspace
 };
 Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     Split s;
+    if (kv8_prompt_wanted(C, Q)) return Split{0, kv8_prompt_tiles(C, Q), false, 0};
     const long rows = (long)Q.queries * (Q.heads / C.heads);
     s.nr = rows > 16 && C.features <= 128 ? 2 : 1;
     s.tiles = (int)((rows + 16 * s.nr - 1) / (16 * s.nr));
@@ -599,6 +519,7 @@ using namespace w4a4;
 extern "C" size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q) {
     if (check(C, Q) || !Q->tokens || !Q->requests || !Q->queries) return 0;
     const Split s = split_of(*C, *Q);
+    if (!s.nr) return kCounters * sizeof(int) + kv8_prompt_workspace_bytes(*C, *Q);
     return s.cut ? kCounters * sizeof(int) + (size_t)s.places * 16 * s.nr * (C->features + 2) * sizeof(float) : 0;
 }
 
@@ -622,6 +543,7 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
                static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
                __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
+    if (!s.nr) return kv8_prompt(a, *C, *Q, po, st);
     auto run = [&](auto bf16, auto d) {
         constexpr bool BF = decltype(bf16)::value;
         constexpr int D = decltype(d)::value;

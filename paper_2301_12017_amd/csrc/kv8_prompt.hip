@@ -1,0 +1,477 @@
+// Attention over the 8-bit cache for many rows: prompts, or what follows an earlier part of one.
+//
+// The mathematics is kv8_attention.hip's (scores transposed, codes as fp16 numbers, queries brought to fp16 by a power of two per
+// row, weights rounded to fp16 with the values' scales in them); the shape is another one.  NW waves of 32 rows share the keys:
+// 64 of them at a time are fetched as codes by all threads, become fp16 numbers ONCE and go to LDS, two buffers in turn,
+// and the 32 x 32 matrix instruction reads them from there.  A lane holds sixteen scores of one row out of 32 keys, the keys
+// 8 (i / 4) + 4 (lane / 32) + i % 4; values are stored in LDS in the order in which that makes the weights the operand of the
+// second product.
+//
+// A weight times its block's scale is one exponential: exp2(raw * k + (log2(v_scale) + c) - m), c a power of two per wave that
+// keeps the largest near 2^6; the row's sum is taken from the same numbers, divided by the scale again, once per sixteen
+// keys.  (A block whose values are 2^40 below the largest block's, or 0, counts in the sum and not in the output.)  The maximum m
+// is let fall behind by up to 2^8 before anything is re-scaled: weights stay below 2^14.
+//
+// Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a maximum, a sum and
+// half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
+// scores (128 features).
+//
+// A group is 32 NW rows of a request and key head.  Groups beyond whole rounds of the device's workgroups are cut into pieces,
+// whose unfinished outputs a second kernel joins, each of its workgroups a slice of a group.
+#include "kv8_attention.hpp"
+
+namespace w4a4 {
+namespace {
+
+constexpr int kMostPieces = 768;                                   // of groups that are cut
+constexpr float kLag = 8.0f;                                       // how far a maximum may fall behind, in powers of two
+
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float16_t mfma32(u32x4_t a, u32x4_t b, float16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+}
+template <typename Op>
+__device__ __forceinline__ float both_halves(float x, Op op) {     // op over the two lanes l, l + 32, in both of them
+    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    return op(__builtin_bit_cast(float, (unsigned)s[0]), __builtin_bit_cast(float, (unsigned)s[1]));
+}
+
+// The work of a call: groups 0 .. whole-1 as they are, then the pieces of the others.  Each wave works it out by itself.
+struct Plan {
+    int per, whole, piece, items;                                  // entries a lane; whole groups; steps of a piece; groups and pieces in all
+    int before, rank;                                              // pieces (or groups) and entries with rows in front of this lane's entries
+    int mine;                                                      // its own
+};
+template <typename Entry>
+__device__ __forceinline__ Plan plan_of(const AttnArgs &a, int entries, Entry entry) {
+    const int lane = threadIdx.x & 63;
+    auto plus = [](int x, int y) { return x + y; };
+    auto in_front = [&](int x) {
+        int upto = x;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += u;
+        }
+        return upto - x;
+    };
+    Plan p;
+    p.per = (entries + 63) / 64;
+    const int e0 = min(lane * p.per, entries), e1 = min(e0 + p.per, entries);
+    int some = 0, most = 0;
+    for (int e = e0; e < e1; ++e) {
+        const int s = entry(e).steps;
+        some += s > 0;
+        most = max(most, s);
+    }
+    p.rank = in_front(some);
+    const int groups = lanes_reduce<64>(some, plus) * a.H, whole_entries = groups / a.slots * a.slots / a.H;
+    most = lanes_reduce<64>(most, [](int x, int y) { return max(x, y); });
+    p.whole = whole_entries * a.H;
+    int rest = 0;
+    for (int e = e0, r = p.rank; e < e1; ++e) {
+        const int s = entry(e).steps;
+        if (s > 0 && r++ >= whole_entries) rest += s;
+    }
+    const float fair = (float)lanes_reduce<64>(rest, plus) * (float)a.H / (float)a.slots;
+    // the size that gets through soonest: rounds of pieces, each of which costs about four steps more (not cut: one round of the longest)
+    p.piece = 0x1000000;
+    float best = (float)most;
+#pragma unroll
+    for (int k = 1; k <= 3; ++k) {
+        const int size = max((int)__builtin_ceilf(fair / (float)k), 4);
+        int n = 0;
+        for (int e = e0, r = p.rank; e < e1; ++e) {
+            const int s = entry(e).steps;
+            if (s > 0 && r++ >= whole_entries) n += pieces_in(s, size);
+        }
+        n = lanes_reduce<64>(n, plus) * a.H;
+        const float cost = (float)((n + a.slots - 1) / a.slots * (size + 4));
+        if (n <= kMostPieces && cost < best) {
+            best = cost;
+            p.piece = size;
+        }
+    }
+    p.mine = 0;
+    for (int e = e0, r = p.rank; e < e1; ++e) {
+        const int s = entry(e).steps;
+        if (s > 0) p.mine += r++ >= whole_entries ? pieces_in(s, p.piece) : 1;
+    }
+    p.before = in_front(p.mine);
+    p.items = lanes_reduce<64>(p.mine, plus) * a.H;
+    return p;
+}
+struct Item { int entry, head, at, pieces; };
+template <typename Entry>
+__device__ __forceinline__ Item item_of(const AttnArgs &a, const Plan &p, int entries, int item, Entry entry) {
+    const int lane = threadIdx.x & 63, owner = __builtin_ctzll(__ballot(item < (p.before + p.mine) * a.H));
+    int before = __builtin_amdgcn_readlane(p.before, owner), rank = __builtin_amdgcn_readlane(p.rank, owner), e = owner * p.per, n = 1;
+    for (; e < entries; ++e) {
+        const int s = entry(e).steps;
+        if (s == 0) continue;
+        n = rank++ * a.H >= p.whole ? pieces_in(s, p.piece) : 1;
+        if (item < (before + n) * a.H) break;
+        before += n;
+    }
+    (void)lane;
+    Item i;
+    const int in = item - before * a.H;
+    i.entry = min(e, entries - 1);
+    i.at = a.heads.of(in);                                         // (the heads of a request side by side)
+    i.head = a.heads.rest(in, i.at);
+    i.pieces = n;
+    return i;
+}
+
+template <int D> constexpr int kPitchK = D + 8;                     // halves of a row in LDS
+template <int D> constexpr int kPitchV = kStep + 8;
+template <int D> constexpr size_t kBuffer = (size_t)(kStep * kPitchK<D> + D * kPitchV<D>) * 2;
+
+template <bool BF16, int D, int NW>
+__global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(AttnArgs a) {
+    constexpr int ROWS = 32 * NW, THREADS = 64 * NW, FT = D / 32, QS = D / 16, N = (4 * D + THREADS - 1) / THREADS, NH = D <= 128 ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[]; // two buffers of [64][keys' row], [D][values' row]
+    __shared__ float s_scale[2][2][4];                             // [buffer][of keys, log2 of values][sixteen keys]; of keys: < 0 for none
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hl = lane >> 5, mask = (1 << a.shift) - 1;
+    const int entries = a.requests * a.tiles.d;
+    auto entry = [&](int e) {
+        const int r = a.tiles.of(e);
+        return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
+    };
+    const Plan plan = plan_of(a, entries, entry);
+    for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
+        const Item it = item_of(a, plan, entries, item, entry);
+        const Tile t = entry(it.entry);
+        const int r = a.tiles.of(it.entry), h = it.head;
+        const int first_step = it.pieces > 1 ? it.at * plan.piece : 0, steps_in = it.pieces > 1 ? min(plan.piece, t.steps - first_step) : t.steps;
+        const int base = (t.begin & ~(kStep - 1)) + first_step * kStep, stop = min(base + steps_in * kStep, t.end);
+        const int steps = stop > base ? (stop - base + kStep - 1) / kStep : 0;
+        const int32_t *ids_of = a.table + (size_t)r * a.width;
+
+        // codes of a step: keys in sixteens of a row, values in sixteens of a feature
+        u32x4_t kreg[N], vreg[N];
+        int kid[N], vid[N];
+        float ks = 0.0f, vs = 0.0f;
+        bool there = false;
+        auto fetch_ids = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = min(tid + i * THREADS, 4 * D - 1), key0 = base + s * kStep;
+                kid[i] = ids_of[min((key0 + c / (D / 16)) >> a.shift, a.width - 1)];
+                vid[i] = ids_of[min((key0 + 16 * (c & 3)) >> a.shift, a.width - 1)];
+            }
+        };
+        auto fetch = [&](int s) {
+            const int key0 = base + s * kStep;
+            if (tid < 4) {
+                const int key = key0 + 16 * tid;
+                there = (key < stop) & (key + 15 >= t.begin) & ((unsigned)vid[0] < (unsigned)a.blocks);
+                const size_t unit = (size_t)(there ? vid[0] : 0) * a.H + h;
+                ks = a.k_scale[unit];
+                vs = a.v_scale[unit];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = min(tid + i * THREADS, 4 * D - 1);
+                const size_t kb = (unsigned)kid[i] < (unsigned)a.blocks ? kid[i] : 0, vb = (unsigned)vid[i] < (unsigned)a.blocks ? vid[i] : 0;
+                const int key = key0 + c / (D / 16), vkey = key0 + 16 * (c & 3);
+                kreg[i] = *reinterpret_cast<const u32x4_t *>(a.k + (((kb * a.H + h) << a.shift) + (key & mask)) * D + c % (D / 16) * 16);
+                vreg[i] = *reinterpret_cast<const u32x4_t *>(a.v + (((vb * a.H + h) * D + (c >> 2)) << a.shift) + (vkey & mask));
+            }
+        };
+        auto put = [&](int buf) {
+            uint16_t *kd = lds + buf * (kBuffer<D> / 2), *vd = kd + kStep * kPitchK<D>;
+            if (tid < 4) {
+                s_scale[buf][0][tid] = there ? ks : -1.0f;
+                s_scale[buf][1][tid] = there && vs > 0.0f ? fmaxf(__builtin_amdgcn_logf(vs), -140.0f) : -300.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = tid + i * THREADS;
+                if (4 * D % THREADS != 0 && c >= 4 * D) break;
+                u32x4_t *k = reinterpret_cast<u32x4_t *>(kd + c / (D / 16) * kPitchK<D> + c % (D / 16) * 16);
+                k[0] = codes8(kreg[i][0], kreg[i][1]);
+                k[1] = codes8(kreg[i][2], kreg[i][3]);
+                // keys 0..3, 8..11 for the lower half of a wave, 4..7, 12..15 for the upper one
+                u32x4_t *v = reinterpret_cast<u32x4_t *>(vd + (c >> 2) * kPitchV<D> + 16 * (c & 3));
+                v[0] = codes8(vreg[i][0], vreg[i][2]);
+                v[1] = codes8(vreg[i][1], vreg[i][3]);
+            }
+        };
+
+        if (steps > 0) {
+            fetch_ids(0);
+            fetch(0);
+            if (steps > 1) fetch_ids(1);
+        }
+        // the lane's row
+        const int wrow = t.row0 + 32 * wave, row = min(wrow + col, t.rows - 1), j = a.group.of(row);
+        const bool any = wrow < t.rows;
+        const int hi = t.len - t.n + j, lo = a.window ? hi - a.window + 1 : 0;
+        const int hi0 = __builtin_amdgcn_readfirstlane(t.len - t.n + a.group.of(min(wrow, t.rows - 1)));
+        const int hi1 = __builtin_amdgcn_readfirstlane(t.len - t.n + a.group.of(min(wrow + 31, t.rows - 1)));
+        const int lo0 = a.window ? hi0 - a.window + 1 : 0, lo1 = a.window ? hi1 - a.window + 1 : 0;
+        u32x4_t q[QS];
+        float back;
+        {
+            const uint16_t *src = a.q + (long)(t.first + j) * a.ldq + (h * a.group.d + a.group.rest(row, j)) * D + 8 * hl;
+#pragma unroll
+            for (int s = 0; s < QS; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(src + 16 * s);
+            float most = 0.0f;
+#pragma unroll
+            for (int s = 0; s < QS; ++s)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    most = fmaxf(most, fmaxf(fabsf(to_float<BF16>((uint16_t)q[s][w])), fabsf(to_float<BF16>((uint16_t)(q[s][w] >> 16)))));
+            most = both_halves(most, max2);
+            const int e = most > 0.0f && most < INFINITY ? max((int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127, -100) : 14;
+            const float up = power(14 - e);
+            back = power(e - 14) * a.scale;
+#pragma unroll
+            for (int s = 0; s < QS; ++s)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    q[s][w] = pack_halves(to_float<BF16>((uint16_t)q[s][w]) * up, to_float<BF16>((uint16_t)(q[s][w] >> 16)) * up);
+        }
+        float16_t o[FT];
+#pragma unroll
+        for (int f = 0; f < FT; ++f) o[f] = float16_t{};
+        float m = -INFINITY, behind = -INFINITY, l = 0.0f, c = 200.0f;          // behind: maximum up to which m is kept
+
+        __syncthreads();                                           // (the last item's keys have been read)
+        if (steps > 0) put(0);
+        if (steps > 1) {
+            fetch(1);
+            if (steps > 2) fetch_ids(2);
+        }
+        __syncthreads();
+        for (int s = 0; s < steps; ++s) {
+            const int buf = s & 1;
+            const uint16_t *kd = lds + buf * (kBuffer<D> / 2) + col * kPitchK<D> + 8 * hl;
+            const uint16_t *vd = lds + buf * (kBuffer<D> / 2) + kStep * kPitchK<D> + col * kPitchV<D> + 8 * hl;
+            float kf[4], ex[4];
+            bool shown = true;
+            float top = -300.0f;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                kf[g] = s_scale[buf][0][g];
+                ex[g] = s_scale[buf][1][g];
+                shown &= kf[g] >= 0.0f;
+                top = fmaxf(top, ex[g]);
+            }
+            if (__builtin_amdgcn_readfirstlane(top + c > 6.0f)) {  // wave-uniform: c follows the scales of values
+                const float by = __builtin_amdgcn_exp2f(4.0f - __builtin_floorf(top) - c);
+                c = 4.0f - __builtin_floorf(top);
+#pragma unroll
+                for (int f = 0; f < FT; ++f)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[f][i] *= by;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) ex[g] = fmaxf(ex[g] + c, -34.0f);
+#pragma unroll
+            for (int part = 0; part < 2; part += NH) {
+                const int key0 = base + s * kStep + 32 * part;
+                if (!any || key0 > hi1 || key0 + 32 * NH - 1 < lo0) continue;           // wave-uniform
+                float16_t x[NH];
+#pragma unroll
+                for (int n = 0; n < NH; ++n) {
+                    x[n] = float16_t{};
+#pragma unroll
+                    for (int i = 0; i < QS; ++i)
+                        x[n] = mfma32(*reinterpret_cast<const u32x4_t *>(kd + 32 * (part + n) * kPitchK<D> + 16 * i), q[i], x[n]);
+                }
+                const bool plain = __builtin_amdgcn_readfirstlane(shown) && key0 + 32 * NH - 1 <= hi0 && key0 >= lo1;
+                if (!plain) {
+#pragma unroll
+                    for (int n = 0; n < NH; ++n)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int key = key0 + 32 * n + 8 * (i / 4) + 4 * hl + i % 4;
+                            x[n][i] = (key <= hi) & (key >= lo) & (kf[2 * (part + n) + i / 8] >= 0.0f) ? x[n][i] : -INFINITY;
+                        }
+                }
+                float by[2 * NH], mx = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < 2 * NH; ++g) {
+                    by[g] = kf[2 * part + g] * back;
+                    float e = x[g / 2][8 * (g % 2)];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) e = fmaxf(e, x[g / 2][8 * (g % 2) + i]);
+                    mx = fmaxf(mx, plain || e > -INFINITY ? e * by[g] : -INFINITY);
+                }
+                mx = both_halves(mx, max2);
+                if (__any(mx > behind)) {                          // seldom after the first steps
+                    const float to = fmaxf(mx, m), a0 = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
+                    m = to;
+                    behind = to + kLag;
+                    l *= a0;
+#pragma unroll
+                    for (int f = 0; f < FT; ++f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[f][i] *= a0;
+                }
+                const float sub = m > -INFINITY ? m : 0.0f;
+                u32x4_t pw[2 * NH];
+#pragma unroll
+                for (int g = 0; g < 2 * NH; ++g) {
+                    const float sh = ex[2 * part + g] - sub;
+                    float p[8], sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float raw = x[g / 2][8 * (g % 2) + i];
+                        float e = __builtin_fmaf(raw, by[g], sh);
+                        if (!plain) e = raw > -INFINITY ? e : -INFINITY;
+                        p[i] = __builtin_amdgcn_exp2f(e);
+                        sum += p[i];
+                    }
+                    l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-ex[2 * part + g]), l);
+                    pw[g] = u32x4_t{pack_halves(p[0], p[1]), pack_halves(p[2], p[3]), pack_halves(p[4], p[5]), pack_halves(p[6], p[7])};
+                }
+#pragma unroll
+                for (int g = 0; g < 2 * NH; ++g)
+#pragma unroll
+                    for (int f = 0; f < FT; ++f)
+                        o[f] = mfma32(*reinterpret_cast<const u32x4_t *>(vd + 32 * f * kPitchV<D> + 16 * (2 * part + g)), pw[g], o[f]);
+            }
+            if (s + 1 < steps) {
+                put(buf ^ 1);
+                if (s + 2 < steps) {
+                    fetch(s + 2);
+                    if (s + 3 < steps) fetch_ids(s + 3);
+                }
+                __syncthreads();
+            }
+        }
+
+        l = both_halves(l, add2);
+        const bool mine = wrow + col < t.rows;
+        const size_t at = ((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(row, j);
+        if (it.pieces > 1) {                                       // [item][wave][four features][lane]: joined later
+            const size_t slot = item - plan.whole;
+            const float down = __builtin_amdgcn_exp2f(-c);
+            if (any) {
+                float4_t *po = reinterpret_cast<float4_t *>(a.po + slot * ROWS * D) + wave * (D / 2) * 16 + lane;
+#pragma unroll
+                for (int f = 0; f < FT; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        po[(4 * f + i) * 64] = float4_t{o[f][4 * i] * down, o[f][4 * i + 1] * down, o[f][4 * i + 2] * down, o[f][4 * i + 3] * down};
+                if (hl == 0) *reinterpret_cast<float2 *>(a.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
+            }
+            continue;
+        }
+        const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(-c) / l : 0.0f;
+        uint16_t *dst = a.out + at * D;
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                auto two = [&](int k) { return (uint32_t)from_float<BF16>(o[f][k] * inv) | (uint32_t)from_float<BF16>(o[f][k + 1] * inv) << 16; };
+                const auto s0 = __builtin_amdgcn_permlane32_swap(two(4 * i), two(4 * i + 4), false, false);
+                const auto s1 = __builtin_amdgcn_permlane32_swap(two(4 * i + 2), two(4 * i + 6), false, false);
+                if (any && mine) *reinterpret_cast<u32x4_t *>(dst + 32 * f + 8 * (i + hl)) = u32x4_t{(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
+            }
+        if (any && mine && hl == 0 && a.lse) a.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+    }
+}
+
+// The pieces of the groups that are cut: the workgroup of piece i of n takes the i-th of n slices of the group.
+template <bool BF16, int D, int NW>
+__global__ __launch_bounds__(256) void kv8_prompt_join_kernel(AttnArgs a) {
+    constexpr int ROWS = 32 * NW, QUADS = NW * (D / 8) * 64;       // fours of features of a row
+    const int entries = a.requests * a.tiles.d;
+    auto entry = [&](int e) {
+        const int r = a.tiles.of(e);
+        return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
+    };
+    const Plan plan = plan_of(a, entries, entry);
+    for (int item = plan.whole + blockIdx.x; item < plan.items; item += gridDim.x) {
+        const Item it = item_of(a, plan, entries, item, entry);
+        if (it.pieces <= 1) continue;
+        const Tile t = entry(it.entry);
+        const size_t slot0 = item - plan.whole - it.at * a.H;      // of the group's first piece; the others are H further each
+        const int share = ((QUADS + it.pieces - 1) / it.pieces + 63) / 64 * 64;
+        for (int i = it.at * share + threadIdx.x; i < min((it.at + 1) * share, QUADS); i += 256) {
+            const int lane = i & 63, k = i / 64 % (D / 8), wave = i / 64 / (D / 8), in = 32 * wave + (lane & 31), row = t.row0 + in;
+            if (row >= t.rows) continue;
+            float m = -INFINITY, l = 0.0f;
+            float4_t y = {0, 0, 0, 0};
+            for (int w = 0; w < it.pieces; ++w) m = fmaxf(m, a.pml[((slot0 + (size_t)w * a.H) * ROWS + in) * 2]);
+#pragma unroll 4
+            for (int w = 0; w < it.pieces; ++w) {
+                const size_t slot = slot0 + (size_t)w * a.H;
+                const float2 ml = *reinterpret_cast<const float2 *>(a.pml + (slot * ROWS + in) * 2);
+                const float4_t v = reinterpret_cast<const float4_t *>(a.po + slot * ROWS * D)[i];
+                const float by = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.0f;
+                l += by * ml.y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += by * v[e];
+            }
+            const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+            const int j = a.group.of(row), d = 32 * (k / 4) + 8 * (k % 4) + 4 * (lane >> 5);
+            const size_t at = ((size_t)(t.first + j) * a.H + it.head) * a.group.d + a.group.rest(row, j);
+            const uint32_t y0 = from_float<BF16>(y[0] * inv) | (uint32_t)from_float<BF16>(y[1] * inv) << 16;
+            const uint32_t y1 = from_float<BF16>(y[2] * inv) | (uint32_t)from_float<BF16>(y[3] * inv) << 16;
+            *reinterpret_cast<u32x2_t *>(a.out + at * D + d) = u32x2_t{y0, y1};
+            if (d == 0 && a.lse) a.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+        }
+    }
+}
+
+int waves_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
+    const long rows = (long)Q.queries * (Q.heads / C.heads);
+    return rows <= 128 || C.features == 256 ? 4 : 8;              // (256 features: a wave's registers leave room for one on a SIMD)
+}
+
+template <bool BF16, int D, int NW>
+int launch(AttnArgs &a, hipStream_t st) {
+    auto kern = kv8_prompt_kernel<BF16, D, NW>;
+    constexpr size_t lds = 2 * kBuffer<D>;
+    static KernelState ks;
+    const void *fn = reinterpret_cast<const void *>(kern);
+    const int cus = prepare_kernel(fn, lds, ks);
+    if (cus < 0) return W4A4_ERR_HIP;
+    const int at_once = resident_per_cu(fn, NW * 64, lds, ks);
+    if (at_once <= 0) return W4A4_ERR_HIP;
+    a.slots = min(kMostPieces, cus * at_once);
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.slots), dim3(NW * 64), lds, st, a);
+    hipLaunchKernelGGL((kv8_prompt_join_kernel<BF16, D, NW>), dim3((unsigned)kMostPieces), dim3(256), 0, st, a);
+    return launch_status();
+}
+
+}  // namespace
+
+bool kv8_prompt_wanted(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) { return (long)Q.queries * (Q.heads / C.heads) > 32; }
+
+int kv8_prompt_tiles(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
+    const int rows = 32 * waves_of(C, Q);
+    return (int)(((long)Q.queries * (Q.heads / C.heads) + rows - 1) / rows);
+}
+
+size_t kv8_prompt_workspace_bytes(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
+    return (size_t)kMostPieces * 32 * waves_of(C, Q) * (C.features + 2) * sizeof(float);
+}
+
+int kv8_prompt(AttnArgs a, const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q, float *parts, hipStream_t st) {
+    const int nw = waves_of(C, Q);
+    a.po = parts;
+    a.pml = parts + (size_t)kMostPieces * 32 * nw * C.features;
+    auto run = [&](auto bf16, auto d) {
+        constexpr bool BF = decltype(bf16)::value;
+        constexpr int D = decltype(d)::value;
+        if constexpr (D <= 128)
+            if (nw == 8) return launch<BF, D, 8>(a, st);
+        return launch<BF, D, 4>(a, st);
+    };
+    auto typed = [&](auto d) { return Q.dtype == W4A4_BF16 ? run(std::true_type{}, d) : run(std::false_type{}, d); };
+    switch (C.features) {
+        case 64: return typed(std::integral_constant<int, 64>{});
+        case 96: return typed(std::integral_constant<int, 96>{});
+        case 128: return typed(std::integral_constant<int, 128>{});
+        default: return typed(std::integral_constant<int, 256>{});
+    }
+}
+
+}  // namespace w4a4
