@@ -10,10 +10,11 @@
 // A weight times its block's scale is one exponential: exp2(raw * k + (log2(v_scale) + c) - m), c a power of two per wave that
 // keeps the largest near 2^6; the row's sum is taken from the same numbers, divided by the scale again, once per sixteen
 // keys.  (A block whose values are 2^40 below the largest block's, or 0, counts in the sum and not in the output.)  The maximum m
-// is let fall behind by up to 2^8 before anything is re-scaled: weights stay below 2^14.
+// is let fall behind by up to 2^8 before what has been summed is re-scaled: weights stay below 2^15.  (To look for weights that are too
+// large among the packed ones, and for a maximum only then, took 207 us where this takes 190.)
 //
-// Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a maximum, a sum and
-// half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
+// Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a sum, half a
+// maximum and half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
 // scores (128 features).
 //
 // A group is 32 NW rows of a request and key head.  Groups beyond whole rounds of the device's workgroups are cut into pieces,
@@ -25,7 +26,6 @@ namespace {
 
 constexpr int kMostPieces = 768;                                   // of groups that are cut
 constexpr float kLag = 8.0f;                                       // how far a maximum may fall behind, in powers of two
-
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float16_t mfma32(u32x4_t a, u32x4_t b, float16_t c) {
@@ -124,23 +124,33 @@ __device__ __forceinline__ Item item_of(const AttnArgs &a, const Plan &p, int en
     return i;
 }
 
+// The arguments of the kernel, read again: what is kept of them in scalar registers from one end of the kernel to the other does not
+// fit and would be moved to and fro in the inner loop.
+__device__ __forceinline__ AttnArgs again() {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttnArgs *)p;
+}
+
 template <int D> constexpr int kPitchK = D + 8;                     // halves of a row in LDS
 template <int D> constexpr int kPitchV = kStep + 8;
 template <int D> constexpr size_t kBuffer = (size_t)(kStep * kPitchK<D> + D * kPitchV<D>) * 2;
 
 template <bool BF16, int D, int NW>
-__global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(AttnArgs args) {
     constexpr int ROWS = 32 * NW, THREADS = 64 * NW, FT = D / 32, QS = D / 16, N = (4 * D + THREADS - 1) / THREADS, NH = D <= 128 ? 2 : 1;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[]; // two buffers of [64][keys' row], [D][values' row]
     __shared__ float s_scale[2][2][4];                             // [buffer][of keys, log2 of values][sixteen keys]; of keys: < 0 for none
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hl = lane >> 5, mask = (1 << a.shift) - 1;
-    const int entries = a.requests * a.tiles.d;
-    auto entry = [&](int e) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hl = lane >> 5, mask = (1 << args.shift) - 1;
+    const int entries = args.requests * args.tiles.d;
+    auto entry_of = [](const AttnArgs &a, int e) {
         const int r = a.tiles.of(e);
         return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
     };
-    const Plan plan = plan_of(a, entries, entry);
+    const Plan plan = plan_of(args, entries, [&](int e) { return entry_of(args, e); });
     for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
+        const AttnArgs a = again();
+        auto entry = [&](int e) { return entry_of(a, e); };
         const Item it = item_of(a, plan, entries, item, entry);
         const Tile t = entry(it.entry);
         const int r = a.tiles.of(it.entry), h = it.head;
@@ -148,6 +158,15 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         const int base = (t.begin & ~(kStep - 1)) + first_step * kStep, stop = min(base + steps_in * kStep, t.end);
         const int steps = stop > base ? (stop - base + kStep - 1) / kStep : 0;
         const int32_t *ids_of = a.table + (size_t)r * a.width;
+        // the lane's chunks in a block: codes of a head lie at head * features * tokens of a block, for keys and for values
+        const uint32_t unit = (uint32_t)(a.H * D) << a.shift;
+        const int8_t *kbase[N], *vbase[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = min(tid + i * THREADS, 4 * D - 1);
+            kbase[i] = a.k + ((size_t)h * D << a.shift) + ((c / (D / 16)) & mask) * D + c % (D / 16) * 16;
+            vbase[i] = a.v + (((size_t)h * D + (c >> 2)) << a.shift) + ((16 * (c & 3)) & mask);
+        }
 
         // codes of a step: keys in sixteens of a row, values in sixteens of a feature
         u32x4_t kreg[N], vreg[N];
@@ -167,17 +186,15 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
             if (tid < 4) {
                 const int key = key0 + 16 * tid;
                 there = (key < stop) & (key + 15 >= t.begin) & ((unsigned)vid[0] < (unsigned)a.blocks);
-                const size_t unit = (size_t)(there ? vid[0] : 0) * a.H + h;
-                ks = a.k_scale[unit];
-                vs = a.v_scale[unit];
+                const size_t at = (size_t)(there ? vid[0] : 0) * a.H + h;
+                ks = a.k_scale[at];
+                vs = a.v_scale[at];
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int c = min(tid + i * THREADS, 4 * D - 1);
-                const size_t kb = (unsigned)kid[i] < (unsigned)a.blocks ? kid[i] : 0, vb = (unsigned)vid[i] < (unsigned)a.blocks ? vid[i] : 0;
-                const int key = key0 + c / (D / 16), vkey = key0 + 16 * (c & 3);
-                kreg[i] = *reinterpret_cast<const u32x4_t *>(a.k + (((kb * a.H + h) << a.shift) + (key & mask)) * D + c % (D / 16) * 16);
-                vreg[i] = *reinterpret_cast<const u32x4_t *>(a.v + (((vb * a.H + h) * D + (c >> 2)) << a.shift) + (vkey & mask));
+                const uint32_t kb = (unsigned)kid[i] < (unsigned)a.blocks ? kid[i] : 0, vb = (unsigned)vid[i] < (unsigned)a.blocks ? vid[i] : 0;
+                kreg[i] = *reinterpret_cast<const u32x4_t *>(kbase[i] + (uint64_t)kb * unit + (key0 & mask) * D);
+                vreg[i] = *reinterpret_cast<const u32x4_t *>(vbase[i] + (uint64_t)vb * unit + (key0 & mask));
             }
         };
         auto put = [&](int buf) {
@@ -250,7 +267,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
             const int buf = s & 1;
             const uint16_t *kd = lds + buf * (kBuffer<D> / 2) + col * kPitchK<D> + 8 * hl;
             const uint16_t *vd = lds + buf * (kBuffer<D> / 2) + kStep * kPitchK<D> + col * kPitchV<D> + 8 * hl;
-            float kf[4], ex[4];
+            float kf[4], ex[4], rv[4];                             // of sixteen keys: their scale, log2 of the weights' factor, 1 / factor
             bool shown = true;
             float top = -300.0f;
 #pragma unroll
@@ -269,71 +286,98 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                     for (int i = 0; i < 16; ++i) o[f][i] *= by;
             }
 #pragma unroll
-            for (int g = 0; g < 4; ++g) ex[g] = fmaxf(ex[g] + c, -34.0f);
+            for (int g = 0; g < 4; ++g) {
+                ex[g] = fmaxf(ex[g] + c, -34.0f);
+                rv[g] = __builtin_amdgcn_exp2f(-ex[g]);
+            }
 #pragma unroll
             for (int part = 0; part < 2; part += NH) {
                 const int key0 = base + s * kStep + 32 * part;
                 if (!any || key0 > hi1 || key0 + 32 * NH - 1 < lo0) continue;           // wave-uniform
+                const bool plain = __builtin_amdgcn_readfirstlane(shown) && key0 + 32 * NH - 1 <= hi0 && key0 >= lo1;
+                // Operands are read from LDS four at a time, while the products of the four before are under way (the compiler by itself reads
+                // each one directly in front of its product and waits for it: a third slower).
+                constexpr int SETS = NH * QS / 4;
                 float16_t x[NH];
 #pragma unroll
-                for (int n = 0; n < NH; ++n) {
-                    x[n] = float16_t{};
+                for (int n = 0; n < NH; ++n) x[n] = float16_t{};
+                u32x4_t kk[2][4];
+                auto key_set = [&](int k) {                        // of each sixteen features: the 32 keys of both halves, or two sixteens
 #pragma unroll
-                    for (int i = 0; i < QS; ++i)
-                        x[n] = mfma32(*reinterpret_cast<const u32x4_t *>(kd + 32 * (part + n) * kPitchK<D> + 16 * i), q[i], x[n]);
+                    for (int u = 0; u < 4; ++u)
+                        kk[k & 1][u] = *reinterpret_cast<const u32x4_t *>(kd + 32 * (part + u % NH) * kPitchK<D> + 16 * (k * (4 / NH) + u / NH));
+                };
+                key_set(0);
+#pragma unroll
+                for (int k = 0; k < SETS; ++k) {
+                    if (k + 1 < SETS) key_set(k + 1);
+                    __builtin_amdgcn_sched_barrier(0x16);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) x[u % NH] = mfma32(kk[k & 1][u], q[k * (4 / NH) + u / NH], x[u % NH]);
                 }
-                const bool plain = __builtin_amdgcn_readfirstlane(shown) && key0 + 32 * NH - 1 <= hi0 && key0 >= lo1;
-                if (!plain) {
+                u32x4_t vv[2][FT];
+                auto value_set = [&](int g) {
 #pragma unroll
-                    for (int n = 0; n < NH; ++n)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int key = key0 + 32 * n + 8 * (i / 4) + 4 * hl + i % 4;
-                            x[n][i] = (key <= hi) & (key >= lo) & (kf[2 * (part + n) + i / 8] >= 0.0f) ? x[n][i] : -INFINITY;
-                        }
-                }
-                float by[2 * NH], mx = -INFINITY;
-#pragma unroll
-                for (int g = 0; g < 2 * NH; ++g) {
-                    by[g] = kf[2 * part + g] * back;
-                    float e = x[g / 2][8 * (g % 2)];
-#pragma unroll
-                    for (int i = 1; i < 8; ++i) e = fmaxf(e, x[g / 2][8 * (g % 2) + i]);
-                    mx = fmaxf(mx, plain || e > -INFINITY ? e * by[g] : -INFINITY);
-                }
-                mx = both_halves(mx, max2);
-                if (__any(mx > behind)) {                          // seldom after the first steps
-                    const float to = fmaxf(mx, m), a0 = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
-                    m = to;
-                    behind = to + kLag;
-                    l *= a0;
-#pragma unroll
-                    for (int f = 0; f < FT; ++f)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[f][i] *= a0;
-                }
-                const float sub = m > -INFINITY ? m : 0.0f;
+                    for (int f = 0; f < FT; ++f) vv[g & 1][f] = *reinterpret_cast<const u32x4_t *>(vd + 32 * f * kPitchV<D> + 16 * (2 * part + g));
+                };
+                value_set(0);
                 u32x4_t pw[2 * NH];
+                auto weigh = [&](auto is_plain) {
+                    constexpr bool PLAIN = decltype(is_plain)::value;
+                    if constexpr (!PLAIN) {
+#pragma unroll
+                        for (int n = 0; n < NH; ++n)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int key = key0 + 32 * n + 8 * (i / 4) + 4 * hl + i % 4;
+                                x[n][i] = (key <= hi) & (key >= lo) & (kf[2 * (part + n) + i / 8] >= 0.0f) ? x[n][i] : -INFINITY;
+                            }
+                    }
+                    float by[2 * NH], mx = -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < 2 * NH; ++g) {
+                        by[g] = kf[2 * part + g] * back;
+                        float e = x[g / 2][8 * (g % 2)];
+#pragma unroll
+                        for (int i = 1; i < 8; ++i) e = fmaxf(e, x[g / 2][8 * (g % 2) + i]);
+                        mx = fmaxf(mx, PLAIN || e > -INFINITY ? e * by[g] : -INFINITY);
+                    }
+                    mx = both_halves(mx, max2);
+                    if (__any(mx > behind)) {                      // the first steps, seldom later; rows that need it
+                        const float to = mx > behind ? fmaxf(mx, m) : m, a0 = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
+                        m = to;
+                        behind = to + kLag;
+                        l *= a0;
+#pragma unroll
+                        for (int f = 0; f < FT; ++f)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[f][i] *= a0;
+                    }
+                    const float sub = m > -INFINITY ? m : 0.0f;
+#pragma unroll
+                    for (int g = 0; g < 2 * NH; ++g) {
+                        const float sh = ex[2 * part + g] - sub;
+                        float p[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float raw = x[g / 2][8 * (g % 2) + i];
+                            float e = __builtin_fmaf(raw, by[g], sh);
+                            if (!PLAIN) e = raw > -INFINITY ? e : -INFINITY;
+                            p[i] = __builtin_amdgcn_exp2f(e);
+                        }
+                        l = __builtin_fmaf(((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])), rv[2 * part + g], l);
+                        pw[g] = u32x4_t{pack_halves(p[0], p[1]), pack_halves(p[2], p[3]), pack_halves(p[4], p[5]), pack_halves(p[6], p[7])};
+                    }
+                };
+                if (plain) weigh(std::true_type{});
+                else weigh(std::false_type{});
 #pragma unroll
                 for (int g = 0; g < 2 * NH; ++g) {
-                    const float sh = ex[2 * part + g] - sub;
-                    float p[8], sum = 0.0f;
+                    if (g + 1 < 2 * NH) value_set(g + 1);
+                    __builtin_amdgcn_sched_barrier(0x16);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float raw = x[g / 2][8 * (g % 2) + i];
-                        float e = __builtin_fmaf(raw, by[g], sh);
-                        if (!plain) e = raw > -INFINITY ? e : -INFINITY;
-                        p[i] = __builtin_amdgcn_exp2f(e);
-                        sum += p[i];
-                    }
-                    l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-ex[2 * part + g]), l);
-                    pw[g] = u32x4_t{pack_halves(p[0], p[1]), pack_halves(p[2], p[3]), pack_halves(p[4], p[5]), pack_halves(p[6], p[7])};
+                    for (int f = 0; f < FT; ++f) o[f] = mfma32(vv[g & 1][f], pw[g], o[f]);
                 }
-#pragma unroll
-                for (int g = 0; g < 2 * NH; ++g)
-#pragma unroll
-                    for (int f = 0; f < FT; ++f)
-                        o[f] = mfma32(*reinterpret_cast<const u32x4_t *>(vd + 32 * f * kPitchV<D> + 16 * (2 * part + g)), pw[g], o[f]);
             }
             if (s + 1 < steps) {
                 put(buf ^ 1);
@@ -346,24 +390,25 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         }
 
         l = both_halves(l, add2);
+        const AttnArgs z = again();
         const bool mine = wrow + col < t.rows;
-        const size_t at = ((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(row, j);
+        const size_t at = ((size_t)(t.first + j) * z.H + h) * z.group.d + z.group.rest(row, j);
         if (it.pieces > 1) {                                       // [item][wave][four features][lane]: joined later
             const size_t slot = item - plan.whole;
             const float down = __builtin_amdgcn_exp2f(-c);
             if (any) {
-                float4_t *po = reinterpret_cast<float4_t *>(a.po + slot * ROWS * D) + wave * (D / 2) * 16 + lane;
+                float4_t *po = reinterpret_cast<float4_t *>(z.po + slot * ROWS * D) + wave * (D / 2) * 16 + lane;
 #pragma unroll
                 for (int f = 0; f < FT; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         po[(4 * f + i) * 64] = float4_t{o[f][4 * i] * down, o[f][4 * i + 1] * down, o[f][4 * i + 2] * down, o[f][4 * i + 3] * down};
-                if (hl == 0) *reinterpret_cast<float2 *>(a.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
+                if (hl == 0) *reinterpret_cast<float2 *>(z.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
             }
             continue;
         }
         const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(-c) / l : 0.0f;
-        uint16_t *dst = a.out + at * D;
+        uint16_t *dst = z.out + at * D;
 #pragma unroll
         for (int f = 0; f < FT; ++f)
 #pragma unroll
@@ -373,13 +418,13 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                 const auto s1 = __builtin_amdgcn_permlane32_swap(two(4 * i + 2), two(4 * i + 6), false, false);
                 if (any && mine) *reinterpret_cast<u32x4_t *>(dst + 32 * f + 8 * (i + hl)) = u32x4_t{(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
             }
-        if (any && mine && hl == 0 && a.lse) a.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+        if (any && mine && hl == 0 && z.lse) z.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
     }
 }
 
 // The pieces of the groups that are cut: the workgroup of piece i of n takes the i-th of n slices of the group.
 template <bool BF16, int D, int NW>
-__global__ __launch_bounds__(256) void kv8_prompt_join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(1024) void kv8_prompt_join_kernel(AttnArgs a) {
     constexpr int ROWS = 32 * NW, QUADS = NW * (D / 8) * 64;       // fours of features of a row
     const int entries = a.requests * a.tiles.d;
     auto entry = [&](int e) {
@@ -393,7 +438,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_join_kernel(AttnArgs a) {
         const Tile t = entry(it.entry);
         const size_t slot0 = item - plan.whole - it.at * a.H;      // of the group's first piece; the others are H further each
         const int share = ((QUADS + it.pieces - 1) / it.pieces + 63) / 64 * 64;
-        for (int i = it.at * share + threadIdx.x; i < min((it.at + 1) * share, QUADS); i += 256) {
+        for (int i = it.at * share + threadIdx.x; i < min((it.at + 1) * share, QUADS); i += 1024) {
             const int lane = i & 63, k = i / 64 % (D / 8), wave = i / 64 / (D / 8), in = 32 * wave + (lane & 31), row = t.row0 + in;
             if (row >= t.rows) continue;
             float m = -INFINITY, l = 0.0f;
@@ -437,7 +482,7 @@ int launch(AttnArgs &a, hipStream_t st) {
     if (at_once <= 0) return W4A4_ERR_HIP;
     a.slots = min(kMostPieces, cus * at_once);
     hipLaunchKernelGGL(kern, dim3((unsigned)a.slots), dim3(NW * 64), lds, st, a);
-    hipLaunchKernelGGL((kv8_prompt_join_kernel<BF16, D, NW>), dim3((unsigned)kMostPieces), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv8_prompt_join_kernel<BF16, D, NW>), dim3((unsigned)cus), dim3(1024), 0, st, a);
     return launch_status();
 }
 
