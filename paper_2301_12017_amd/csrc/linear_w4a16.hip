@@ -12,10 +12,11 @@
 // a group, and every 128 codes at the latest: with the offset in them they are up to 50 times larger than the result.
 //
 // A wave holds NT tiles of 16 channels x MT of 16 tokens and reads chunks of 128 codes of K, 16 bytes (32 codes) a lane, straight
-// into registers; the waves of a workgroup take turns over K and add up through LDS.  The order of K inside an instruction
-// is free as long as both operands agree: (w >> 4j) & 0x000F000F gives codes j and j + 4 of a word, so the pairs of x are
-// put in that order.  Groups that are not whole chunks (32, 64, 96, ...): the four words of the four lanes that share a row
-// change places (two lane swaps a pair), so that each instruction reads 32 consecutive codes and a sum never crosses a group.
+// into registers, codes two chunks ahead and x, which comes out of L2, one; the waves of a workgroup have a part of K each, which they add up through LDS.  The four
+// words of the four lanes that share a row then change places (two lane swaps a pair), so that each instruction takes 32 consecutive
+// codes: a sum never crosses a group (of any multiple of 32), and a row of x is read 64 bytes at a time (without the swaps its
+// four lanes read 64 bytes apart, 32 cache lines a load instead of 16).  Inside eight codes the order is free as long as both
+// operands agree: (w >> 4j) & 0x000F000F gives codes j and j + 4 of a word, so the pairs of x are put in that order.
 #include "gen.hpp"
 
 namespace w4a4 {
@@ -52,21 +53,24 @@ __device__ __forceinline__ u32x4_t codes8(uint32_t w) {
     return u32x4_t{(w & 0x000F000Fu) | kOr, ((w >> 4) & 0x000F000Fu) | kOr, ((w >> 8) & 0x000F000Fu) | kOr, ((w >> 12) & 0x000F000Fu) | kOr};
 }
 
+struct __attribute__((packed, aligned(4))) Floats4 { float v[4]; };   // (rows of scales begin at any float)
+
 // SMALL: groups that are not a multiple of 128 codes.
-template <bool BF16, bool ASYM, bool SMALL, int MT, int NT, int NW, int PF>
-__global__ __launch_bounds__(NW * 64) void linear_w4a16_kernel(W4A16Args a) {
+template <bool BF16, bool ASYM, bool SMALL, int MT, int NT, int NW>
+__global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args a) {
     extern __shared__ float red[];                                 // [NW][MT * NT * 4][64]
-    constexpr int FOLDS = SMALL ? 4 : 1;                           // sums per chunk that get a scale of their own
+    constexpr int FOLDS = SMALL ? 4 : 1, AHEAD = 2;                // sums per chunk that get a scale of their own; chunks requested ahead
     constexpr uint32_t kOne = BF16 ? 0x3F803F80u : 0x3C003C00u;
     constexpr uint32_t kOff = BF16 ? 0xC308C308u : 0x80088008u;    // -136; -8 * 2^-24
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
     const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT);
-    const int chunks = (a.K + 127) >> 7;
+    const int chunks = (a.K + 127) >> 7, each = (chunks + NW - 1) / NW, c0 = wave * each, c1 = min(c0 + each, chunks);
 
+    // (x of rows behind the last one keeps what the registers hold)
     struct Stage {
-        u32x4_t w[NT], x[MT][4];
-        float s[NT][FOLDS], z[NT][ASYM ? FOLDS : 1];
-    } st[PF];
+        u32x4_t w[NT];
+        float s[NT][SMALL ? 4 : 1], z[NT][SMALL && ASYM ? 4 : 1];  // (small groups)
+    } st[AHEAD];
     const uint8_t *wp[NT];
     const float *sp[NT], *zp[NT];
 #pragma unroll
@@ -76,34 +80,88 @@ __global__ __launch_bounds__(NW * 64) void linear_w4a16_kernel(W4A16Args a) {
         sp[t] = a.scale + (size_t)n * a.ng;
         if (ASYM) zp[t] = a.zero + (size_t)n * a.ng;
     }
+    u32x4_t x[MT][4];
     const uint16_t *xp[MT];
+    bool on[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xp[t] = a.x + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.ldx;
+    for (int t = 0; t < MT; ++t) {
+        const int m = m0 + 16 * t + col;
+        on[t] = m < a.M;
+        xp[t] = a.x + (size_t)(on[t] ? m : 0) * a.ldx + 8 * kg;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[t][j] = u32x4_t{0, 0, 0, 0};
+    }
+    float s4[NT][4], z4[NT][4];                                    // groups of whole chunks: the scales of four
+    auto load4 = [&](int c) {                                      // of chunks c .. c + 3
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (a.group == 128 && c + 3 < a.ng) {
+                const Floats4 f = *reinterpret_cast<const Floats4 *>(sp[t] + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s4[t][j] = f.v[j];
+                if (ASYM) {
+                    const Floats4 g = *reinterpret_cast<const Floats4 *>(zp[t] + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) z4[t][j] = g.v[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int g = a.group ? min(128 * (c + j) / a.group, a.ng - 1) : 0;
+                    s4[t][j] = sp[t][g];
+                    if (ASYM) z4[t][j] = zp[t][g];
+                }
+            }
+        }
+    };
 
     auto load = [&](Stage &s, int c) {
         const int left = a.K - 128 * c;                            // codes from here on: below 128 in the last chunk only
-        const bool in = 32 * kg < left;
-        const int wo = 64 * c + (in ? 16 * kg : 0);
+        const int wo = 64 * c + (32 * kg < left ? 16 * kg : 0);
 #pragma unroll
         for (int t = 0; t < NT; ++t) s.w[t] = *reinterpret_cast<const u32x4_t *>(wp[t] + wo);
+        if constexpr (SMALL) {
+            if (a.group == 32 && 4 * c + 3 < a.ng) {
 #pragma unroll
-        for (int f = 0; f < FOLDS; ++f) {
-            const int k = 128 * c + 32 * f;
-            const int g = a.group && k < a.K ? k / a.group : 0;
+                for (int t = 0; t < NT; ++t) {
+                    const Floats4 f = *reinterpret_cast<const Floats4 *>(sp[t] + 4 * c);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                s.s[t][f] = sp[t][g];
-                if (ASYM) s.z[t][f] = zp[t][g];
+                    for (int j = 0; j < 4; ++j) s.s[t][j] = f.v[j];
+                    if constexpr (ASYM) {
+                        const Floats4 g = *reinterpret_cast<const Floats4 *>(zp[t] + 4 * c);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s.z[t][j] = g.v[j];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const int g = min((128 * c + 32 * f) / a.group, a.ng - 1);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        s.s[t][f] = sp[t][g];
+                        if constexpr (ASYM) s.z[t][f] = zp[t][g];
+                    }
+                }
             }
         }
+    };
+    auto load_x = [&](int c) {
+        const int left = a.K - 128 * c;
+        if (left >= 128) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = SMALL ? 32 * j + 8 * kg : 32 * kg + 8 * j;
+            for (int t = 0; t < MT; ++t)
+                if (on[t])
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                s.x[t][j] = u32x4_t{0, 0, 0, 0};
-                if (k < left) s.x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + k);
-            }
+                    for (int j = 0; j < 4; ++j) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + 32 * j);
+        } else {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[t][j] = u32x4_t{0, 0, 0, 0};
+                    if (32 * j < left) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + 32 * j);
+                }
         }
     };
 
@@ -113,62 +171,75 @@ __global__ __launch_bounds__(NW * 64) void linear_w4a16_kernel(W4A16Args a) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) tot[i][t] = float4_t{0, 0, 0, 0};
 
-    auto compute = [&](Stage &s) {
-        if (SMALL)
+    auto compute = [&](Stage &s, int next, auto scale, auto zero) {
+        u32x4_t xr[MT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s.w[t] = transpose_groups(s.w[t]);
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int f = 0; f < FOLDS; ++f) {
-            constexpr int STEPS = 4 / FOLDS;
-            u32x4_t xr[MT][STEPS];
-            float4_t first[MT], sx[MT];
+            for (int j = 0; j < 4; ++j) xr[i][j] = pair_up(x[i][j]);
+        __builtin_amdgcn_sched_barrier(0);                         // (else their registers are needed twice)
+        if (next < c1) load_x(next);
+        constexpr int STEPS = 4 / FOLDS;
+        float4_t first[FOLDS][MT], sx[FOLDS][MT];
+#pragma unroll
+        for (int f = 0; f < FOLDS; ++f)
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                first[i] = sx[i] = float4_t{0, 0, 0, 0};
+                first[f][i] = sx[f][i] = float4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int j = 0; j < STEPS; ++j) {
-                    xr[i][j] = pair_up(s.x[i][f * STEPS + j]);
-                    if (ASYM) sx[i] = mfma16<BF16>(xr[i][j], u32x4_t{kOne, kOne, kOne, kOne}, sx[i]);
-                    else first[i] = mfma16<BF16>(xr[i][j], u32x4_t{kOff, kOff, kOff, kOff}, first[i]);
+                    if (ASYM) sx[f][i] = mfma16<BF16>(xr[i][f * STEPS + j], u32x4_t{kOne, kOne, kOne, kOne}, sx[f][i]);
+                    else first[f][i] = mfma16<BF16>(xr[i][f * STEPS + j], u32x4_t{kOff, kOff, kOff, kOff}, first[f][i]);
                 }
-                if (ASYM && BF16)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) first[i][e] = -128.0f * sx[i][e];
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t) {
+            const u32x4_t w4 = transpose_groups(s.w[t]);
+#pragma unroll
+            for (int f = 0; f < FOLDS; ++f) {
                 float4_t acc[MT];
 #pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i] = first[i];
+                for (int i = 0; i < MT; ++i) {
+                    acc[i] = first[f][i];
+                    if (ASYM && BF16)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][e] = -128.0f * sx[f][i][e];
+                }
 #pragma unroll
                 for (int j = 0; j < STEPS; ++j) {
-                    const u32x4_t w = codes8<BF16, ASYM>(s.w[t][f * STEPS + j]);
+                    const u32x4_t w = codes8<BF16, ASYM>(w4[f * STEPS + j]);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i] = mfma16<BF16>(xr[i][j], w, acc[i]);
+                    for (int i = 0; i < MT; ++i) acc[i] = mfma16<BF16>(xr[i][f * STEPS + j], w, acc[i]);
                 }
-                const float sc = BF16 ? s.s[t][f] : s.s[t][f] * 16777216.0f;
+                const float sc = BF16 ? scale(t, f) : scale(t, f) * 16777216.0f;
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         tot[i][t][e] = __fmaf_rn(acc[i][e], sc, tot[i][t][e]);
-                        if (ASYM) tot[i][t][e] = __fmaf_rn(sx[i][e], s.z[t][f], tot[i][t][e]);
+                        if (ASYM) tot[i][t][e] = __fmaf_rn(sx[f][i][e], zero(t, f), tot[i][t][e]);
                     }
             }
+            if (NT > 1) __builtin_amdgcn_sched_barrier(0);
         }
     };
 
+    if (c0 < c1) {
+        if (!SMALL) load4(c0);
 #pragma unroll
-    for (int p = 0; p < PF; ++p)
-        if (wave + p * NW < chunks) load(st[p], wave + p * NW);
-    for (int c = wave; c < chunks; c += PF * NW) {
+        for (int p = 0; p < AHEAD; ++p)
+            if (c0 + p < c1) load(st[p], c0 + p);
+        load_x(c0);
+        for (int c = c0; c < c1; c += 4) {
 #pragma unroll
-        for (int p = 0; p < PF; ++p) {
-            const int at = c + p * NW;
-            if (at < chunks) {
-                compute(st[p]);
-                if (at + PF * NW < chunks) load(st[p], at + PF * NW);
+            for (int j = 0; j < 4; ++j) {
+                if (c + j >= c1) break;
+                Stage &s = st[j % AHEAD];
+                if constexpr (SMALL) compute(s, c + j + 1, [&](int t, int f) { return s.s[t][f]; }, [&](int t, int f) { return s.z[t][f]; });
+                else compute(s, c + j + 1, [&](int t, int) { return s4[t][j]; }, [&](int t, int) { return z4[t][j]; });
+                if (c + j + AHEAD < c1) load(s, c + j + AHEAD);
             }
+            if (!SMALL && a.group && c + 4 < c1) load4(c + 4);
         }
     }
 
@@ -194,9 +265,9 @@ __global__ __launch_bounds__(NW * 64) void linear_w4a16_kernel(W4A16Args a) {
     }
 }
 
-template <bool BF16, bool ASYM, bool SMALL, int MT, int NT, int NW, int PF>
+template <bool BF16, bool ASYM, bool SMALL, int MT, int NT, int NW>
 int launch(const W4A16Args &a, hipStream_t st) {
-    auto kern = linear_w4a16_kernel<BF16, ASYM, SMALL, MT, NT, NW, PF>;
+    auto kern = linear_w4a16_kernel<BF16, ASYM, SMALL, MT, NT, NW>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     static KernelState ks;
     if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
@@ -205,11 +276,24 @@ int launch(const W4A16Args &a, hipStream_t st) {
     return launch_status();
 }
 
+// Tiles of channels a wave: as many as leave a workgroup for three quarters of the CUs (x is read once per workgroup, and costs as many
+// load instructions as the codes of four tiles; more tiles than that leave CUs without work).  us at one | two | four tiles, N x K:
+//   1 token 16000 x 4096 13.0 | 10.7 | 10.8, 5 tokens 4096 x 4096 5.4 | 6.3 | 9.6, 16 tokens 16000 x 11008 58 | 40 | 32,
+//   32 tokens 16384 x 4096 41 | 25 | 17.6, 20 tokens 4096 x 4096 8.5 | 9.8 | 13.4, 64 tokens 16000 x 4096 71 | 42 | 29.
+// Four tiles of four times sixteen tokens take the registers of a SIMD for one wave.  Small groups have four sums a chunk, whose
+// operands leave room for one tile (24 tokens 2000 x 8000 in groups of 32: 17 us, two tiles 47), for two where tokens are few.
+template <bool BF16, bool ASYM, bool SMALL, int MT>
+int pick(const W4A16Args &a, hipStream_t st) {
+    const int tiles = a.N / 16;
+    if constexpr (!SMALL)
+        if (tiles >= 4 * 192) return launch<BF16, ASYM, SMALL, MT, 4, MT == 4 ? 4 : 8>(a, st);
+    if constexpr (!SMALL || MT == 1)
+        if (tiles >= 2 * 192) return launch<BF16, ASYM, SMALL, MT, 2, MT == 4 ? 4 : 8>(a, st);
+    return launch<BF16, ASYM, SMALL, MT, 1, 8>(a, st);
+}
 template <bool BF16, bool ASYM, bool SMALL>
 int pick(const W4A16Args &a, hipStream_t st) {
-    if (a.M <= 16) return a.N >= 8192 ? launch<BF16, ASYM, SMALL, 1, 2, 8, 2>(a, st) : launch<BF16, ASYM, SMALL, 1, 1, 8, 2>(a, st);
-    if (a.M <= 32) return a.N >= 8192 ? launch<BF16, ASYM, SMALL, 2, 4, 4, 2>(a, st) : launch<BF16, ASYM, SMALL, 2, 1, 8, 2>(a, st);
-    return a.N >= 8192 ? launch<BF16, ASYM, SMALL, 4, 4, 4, 1>(a, st) : launch<BF16, ASYM, SMALL, 4, 1, 8, 1>(a, st);
+    return a.M <= 16 ? pick<BF16, ASYM, SMALL, 1>(a, st) : a.M <= 32 ? pick<BF16, ASYM, SMALL, 2>(a, st) : pick<BF16, ASYM, SMALL, 4>(a, st);
 }
 
 }  // namespace
