@@ -293,7 +293,10 @@ int pick(const W4A16Args &a, hipStream_t st) {
 }
 template <bool BF16, bool ASYM, bool SMALL>
 int pick(const W4A16Args &a, hipStream_t st) {
-    return a.M <= 16 ? pick<BF16, ASYM, SMALL, 1>(a, st) : a.M <= 32 ? pick<BF16, ASYM, SMALL, 2>(a, st) : pick<BF16, ASYM, SMALL, 4>(a, st);
+    if (a.M <= 16) return pick<BF16, ASYM, SMALL, 1>(a, st);
+    if constexpr (!SMALL)
+        if (a.M > 32) return pick<BF16, ASYM, SMALL, 4>(a, st);
+    return pick<BF16, ASYM, SMALL, 2>(a, st);
 }
 
 }  // namespace
