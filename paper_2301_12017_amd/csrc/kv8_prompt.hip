@@ -173,12 +173,15 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         int kid[N], vid[N];
         float ks = 0.0f, vs = 0.0f;
         bool there = false;
+        auto id_of = [&](int key) {                                // (a 32-bit offset from a uniform address)
+            return *reinterpret_cast<const int32_t *>(reinterpret_cast<const char *>(ids_of) + 4u * (uint32_t)min(key >> a.shift, a.width - 1));
+        };
         auto fetch_ids = [&](int s) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int c = min(tid + i * THREADS, 4 * D - 1), key0 = base + s * kStep;
-                kid[i] = ids_of[min((key0 + c / (D / 16)) >> a.shift, a.width - 1)];
-                vid[i] = ids_of[min((key0 + 16 * (c & 3)) >> a.shift, a.width - 1)];
+                kid[i] = id_of(key0 + c / (D / 16));
+                vid[i] = id_of(key0 + 16 * (c & 3));
             }
         };
         auto fetch = [&](int s) {
@@ -290,6 +293,13 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                 ex[g] = fmaxf(ex[g] + c, -34.0f);
                 rv[g] = __builtin_amdgcn_exp2f(-ex[g]);
             }
+            if (s + 1 < steps) {                                   // (the other buffer's step is over for every wave)
+                put(buf ^ 1);
+                if (s + 2 < steps) {
+                    fetch(s + 2);
+                    if (s + 3 < steps) fetch_ids(s + 3);
+                }
+            }
 #pragma unroll
             for (int part = 0; part < 2; part += NH) {
                 const int key0 = base + s * kStep + 32 * part;
@@ -379,14 +389,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                     for (int f = 0; f < FT; ++f) o[f] = mfma32(vv[g & 1][f], pw[g], o[f]);
                 }
             }
-            if (s + 1 < steps) {
-                put(buf ^ 1);
-                if (s + 2 < steps) {
-                    fetch(s + 2);
-                    if (s + 3 < steps) fetch_ids(s + 3);
-                }
-                __syncthreads();
-            }
+            if (s + 1 < steps) __syncthreads();
         }
 
         l = both_halves(l, add2);
