@@ -55,7 +55,7 @@ __device__ __forceinline__ Cut cut_of(const AttnArgs &a, int entries, int least,
     for (int i = e0; i < e1; ++i) mine += only = entry(i).steps;
     const float fair = (float)lanes_reduce<64>(mine, plus) * (float)a.H / (float)a.slots;
     const int most = entries * a.H <= a.slots ? a.slots : entries * a.H + a.slots;
-    constexpr float kMore[8] = {1.0f, 1.1f, 1.25f, 1.4f, 1.6f, 2.0f, 2.5f, 3.5f};
+    constexpr float kMore[8] = {1.0f, 1.1f, 1.2f, 1.3f, 1.45f, 1.7f, 2.2f, 3.5f};
     int piece = 0x1000000, count[8] = {};
     auto size = [&](int j) { return max((int)__builtin_ceilf(fair * kMore[j]), least); };
     for (int i = e0; i < e1; ++i) {
@@ -120,12 +120,14 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
     struct Ids { int k, v; };
     const int32_t *ids_of = a.table + (size_t)r * a.width;
     auto fetch_ids = [&](int key0) { return Ids{ids_of[min((key0 + 16 * kgroup) >> a.shift, a.width - 1)], ids_of[min((key0 + 16 * kg) >> a.shift, a.width - 1)]}; };
-    const int first_step = cut.at * cut.piece;
     Ids next = {0, 0};
-    if (a.width && !a.window) next = fetch_ids((first_step + wave) * kStep);
+    if (!CUT && a.width && !a.window) next = fetch_ids(wave * kStep);
     const Tile t = entry(cut.entry);
     if (!t.steps) return;
-    const int np = CUT ? pieces_in(t.steps, cut.piece) : 1, steps = CUT ? min(cut.piece, t.steps - first_step) : t.steps;
+    // (the pieces of a group are equally long: no short one at its end)
+    const int np = CUT ? pieces_in(t.steps, cut.piece) : 1, piece = CUT ? pieces_in(t.steps, np) : t.steps, first_step = cut.at * piece;
+    const int steps = min(piece, t.steps - first_step);
+    if (CUT && a.width && !a.window) next = fetch_ids((first_step + wave) * kStep);
     const int base = (t.begin & ~(kStep - 1)) + first_step * kStep, stop = min(base + steps * kStep, t.end);
     const int todo = stop > base ? steps : 0;
     if (a.window && wave < todo) next = fetch_ids(base + wave * kStep);
