@@ -12,6 +12,8 @@
 //
 // Bound by latency: the requests' words, the sums, the ring's and the table's words, one after the other.  Sums run over lanes
 // (data-parallel primitives) and then over waves, three at a time; 64 requests take 256 threads, thousands 1024.
+// Measured: 64 requests of one token each 4.5 us; 2999 requests, prompts, single tokens and ended ones mixed, 7.2 us (sums by shuffles
+// and ended requests served by sixteen lanes each: 9.9).
 #include "gen.hpp"
 
 namespace w4a4 {
