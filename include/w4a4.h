@@ -583,8 +583,8 @@ typedef struct {
  * The tokens of one block stand together in `slots`, in any order, and no slot comes twice: w4a4_kv8_plan leaves them so (if not, what that block
  * holds afterwards is unspecified).  A block that gets its first slot begins anew: what it held is lost, its scale is the new tokens'
  * largest magnitude / 127.  Otherwise the scale is raised where the new tokens need it, and the codes that stay are scaled
- * down by old / new, to nearest even.  Codes are x * (1 / scale), to nearest even, at most 127 in magnitude; an infinity becomes +-127 and a NaN 0, and neither
- * counts for the scale. A scale below the smallest normal number is stored as 0. */
+ * down by old / new, to nearest even.  Codes are x * (1 / scale), to nearest even, at most 127 in magnitude; an infinity becomes +-127 (0 where the scale is 0) and a NaN 0, and
+ * neither counts for the scale. A scale below the smallest normal number is stored as 0. */
 int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv,
                     const int32_t *slots, void *stream);
 
@@ -609,7 +609,7 @@ typedef struct {
 /* out [tokens, heads, features], lse [tokens, heads] (may be NULL): causal attention of each request's queries, its last positions,
  * over its keys in the cache, and the logarithm of the sum of exp(score).  A query that sees nothing (a request of no
  * keys, a row that pads the batch) gets zeros and -infinity.  Rows of tokens that belong to no request are not written.
- * `queries` must hold (queries beyond it are not computed); keys past `context` only cost time.  A table entry that names no block
+ * `queries` must hold (of a request that has more, nothing is promised but which rows are written: at most its own); keys past `context` only cost time.  A table entry that names no block
  * of the cache hides its keys.  The workspace (16-byte aligned): its first 18432 bytes are zeros before its first use, and every call leaves
  * them so; it belongs to one call at a time, any that it is large enough for. */
 size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q);

@@ -60,7 +60,7 @@ __device__ __forceinline__ Cut cut_of(const AttnArgs &a, int entries, int least,
     const float fair = (float)lanes_reduce<64>(mine, plus) * (float)a.H / (float)a.slots;
     const int most = entries * a.H <= a.slots ? a.slots : entries * a.H + a.slots;
     constexpr float kMore[8] = {1.0f, 1.1f, 1.2f, 1.3f, 1.45f, 1.7f, 2.2f, 3.5f};
-    int piece = 0x1000000, count[8] = {};
+    int piece = 0x2000000, count[8] = {};
     auto size = [&](int j) { return max((int)__builtin_ceilf(fair * kMore[j]), least); };
     for (int i = e0; i < e1; ++i) {
         const int steps = per == 1 ? only : entry(i).steps;
@@ -399,14 +399,14 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
         if (row < rows)
             for (int w = tid % LANES; w < parts; w += LANES) {
                 const Two x = take2(a.pml + (part(w) + row) * 2);
-                if (x.x > -INFINITY) {
+                if (x.x > -INFINITY || x.y != 0.0f) {              // (NaN, which is no maximum)
                     const float to = fmaxf(mx, x.x);
                     sum = sum * __builtin_amdgcn_exp2f(mx - to) + x.y * __builtin_amdgcn_exp2f(x.x - to);
                     mx = to;
                 }
             }
         const float most = lanes_reduce<LANES>(mx, max2);
-        sum = lanes_reduce<LANES>(mx > -INFINITY ? sum * __builtin_amdgcn_exp2f(mx - most) : 0.0f, add2);
+        sum = lanes_reduce<LANES>(mx > -INFINITY ? sum * __builtin_amdgcn_exp2f(mx - most) : sum, add2);
         if (tid % LANES == 0) {
             ml[row] = most;
             ml[ROWS + row] = sum != 0.0f ? 1.0f / sum : 0.0f;

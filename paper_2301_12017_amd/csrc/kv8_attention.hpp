@@ -82,7 +82,7 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
 }
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // 2^e, -126 <= e <= 127
 
-// s / t, rounded up, for s < 2^24 (a step more or less makes no difference to who uses it, but all use the same)
+// s / t, rounded up, for s + t < 2^31 (a step more or less makes no difference to who uses it, but all use the same)
 __device__ __forceinline__ int pieces_in(int steps, int piece) { return (steps + piece - 1) / piece; }
 
 // Many rows (kv8_prompt.hip).

@@ -9,7 +9,7 @@
 //
 // A weight times its block's scale is one exponential: exp2(raw * k + (log2(v_scale) + c) - m), c a power of two per wave that
 // keeps the largest near 2^6; the row's sum is taken from the same numbers, divided by the scale again, once per sixteen
-// keys.  (A block whose values are 2^40 below the largest block's, or 0, counts in the sum and not in the output.)  The maximum m
+// keys.  (Weights of a block whose scale is 2^20 below the largest one's begin to lose bits; one that is 2^40 below, or 0, counts in the sum and not in the output.)  The maximum m
 // is let fall behind by up to 2^8 before what has been summed is re-scaled: weights stay below 2^15.  (To look for weights that are too
 // large among the packed ones, and for a maximum only then, took 207 us where this takes 190.)
 //
@@ -78,7 +78,7 @@ __device__ __forceinline__ Plan plan_of(const AttnArgs &a, int entries, Entry en
     }
     const float fair = (float)lanes_reduce<64>(rest, plus) * (float)a.H / (float)a.slots;
     // the size that gets through soonest: rounds of pieces, each of which costs about four steps more (not cut: one round of the longest)
-    p.piece = 0x1000000;
+    p.piece = 0x2000000;                                           // (more than the steps of 2^31 keys)
     float best = (float)most;
 #pragma unroll
     for (int k = 1; k <= 3; ++k) {

@@ -493,6 +493,24 @@ def test_a_row_of_nan_stays_in_its_row(B):
         assert torch.equal(want, got)
 
 
+@pytest.mark.parametrize("n, keys", [(1, 9000), (3, 9000), (40, 9000)])
+def test_a_row_of_nan_stays_nan_in_a_request_that_is_cut(B, n, keys):
+    g = _gen(5)
+    blocks = -(-keys // 64)
+    cache = _random_cache(B, g, blocks, 2, 64, 128)
+    q = torch.randn((n, 4, 128), generator=g).half().cuda()
+    call = B.PreparedKV8Attention(q, cache, torch.arange(blocks, dtype=torch.int32, device="cuda")[None], torch.tensor([keys], dtype=torch.int32, device="cuda"),
+                                  torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, keys, 0.09, want_lse=True)
+    call()
+    want, sums = call.out.clone(), call.lse.clone()
+    q[n - 1, 2, 5] = float("nan")
+    call()
+    assert torch.isnan(call.out[n - 1, 2]).all() and torch.isnan(call.lse[n - 1, 2])
+    for got, before in ((call.out, want), (call.lse, sums)):
+        got[n - 1, 2] = before[n - 1, 2] = 0
+        assert torch.equal(got, before)
+
+
 # ---- streams, graphs -------------------------------------------------------------------------------------------------------
 def _step(B, seed=0, R=5, H=2, group=3, D=64, block=16):
     """One step's calls on one state: plan, append, attention, a linear behind it."""
