@@ -547,7 +547,7 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     float *po = reinterpret_cast<float *>(arrived + (need ? kCounters : 0));
     AttnArgs a{static_cast<const uint16_t *>(Q->q), C->k, C->v, C->k_scale, C->v_scale, Q->table, Q->lens, Q->start,
                static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
-               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
+               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, 0x7fffffff, Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
     if (!s.nr) return kv8_prompt(a, *C, *Q, po, st);
     auto run = [&](auto bf16, auto d) {

@@ -28,22 +28,29 @@ struct AttnArgs {
     int *arrived;
     long ldq;
     int tokens, blocks, H, shift, width, window, queries, requests, slots;
+    int least, most;                                               // rows of a request that this kernel takes; others are another's
     Div group, tiles, heads;                                       // queries of a head of the cache; tiles of a request; = H
     float scale;                                                   // in powers of two: scale / ln 2
 };
 
+// Queries (0 where another kernel takes them) and keys of a request.
+struct Sizes { int n, len; };
+__device__ __forceinline__ Sizes sizes_of(const AttnArgs &a, int r) {
+    const int n = max(min(min(a.start[r + 1], a.tokens) - max(a.start[r], 0), a.queries), 0), rows = n * a.group.d;
+    return Sizes{rows >= a.least && rows <= a.most ? n : 0, min(max(a.lens[r], 0), (int)min((long)a.width << a.shift, 0x7fffff00L))};
+}
 // The rows of a group and the keys they see.
 struct Tile {
     int first, n, len, rows, row0;                                 // first token, queries, keys of the request; rows of it; this tile's first
     int begin, end;                                                // keys that any row of the tile sees
     int steps;                                                     // 0: no rows; else one at least
 };
-__device__ __forceinline__ Tile tile_of(const AttnArgs &a, int r, int row0, int tile) {
+__device__ __forceinline__ Tile tile_of(const AttnArgs &a, Sizes s, int row0, int tile) {
     Tile t;
-    t.first = max(a.start[r], 0);
-    t.n = min(min(a.start[r + 1], a.tokens) - t.first, a.queries);
-    t.rows = t.n > 0 ? t.n * a.group.d : 0;
-    t.len = min(max(a.lens[r], 0), (int)min((long)a.width << a.shift, 0x7fffff00L));
+    t.first = 0;
+    t.n = s.n;
+    t.len = s.len;
+    t.rows = s.n * a.group.d;
     t.row0 = row0;
     t.begin = t.end = t.steps = 0;
     if (row0 < t.rows) {
@@ -52,6 +59,11 @@ __device__ __forceinline__ Tile tile_of(const AttnArgs &a, int r, int row0, int 
         t.begin = a.window ? min(max(lo - a.window + 1, 0), t.end) : 0;
         t.steps = t.end > t.begin ? (t.end - (t.begin & ~(kStep - 1)) + kStep - 1) / kStep : 1;
     }
+    return t;
+}
+__device__ __forceinline__ Tile tile_of(const AttnArgs &a, int r, int row0, int tile) {
+    Tile t = tile_of(a, sizes_of(a, r), row0, tile);
+    t.first = max(a.start[r], 0);
     return t;
 }
 

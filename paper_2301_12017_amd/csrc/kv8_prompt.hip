@@ -39,91 +39,113 @@ __device__ __forceinline__ float both_halves(float x, Op op) {     // op over th
     return op(__builtin_bit_cast(float, (unsigned)s[0]), __builtin_bit_cast(float, (unsigned)s[1]));
 }
 
+__device__ __forceinline__ int upto_lane(int x) {                  // sum over the lanes up to this one
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(x, o, 64);
+        if (lane >= o) x += u;
+    }
+    return x;
+}
+
 // The work of a call: groups 0 .. whole-1 as they are, then the pieces of the others.  Each wave works it out by itself.
 struct Plan {
     int per, whole, piece, items;                                  // entries a lane; whole groups; steps of a piece; groups and pieces in all
     int before, rank;                                              // pieces (or groups) and entries with rows in front of this lane's entries
     int mine;                                                      // its own
 };
-template <typename Entry>
-__device__ __forceinline__ Plan plan_of(const AttnArgs &a, int entries, Entry entry) {
+// f(steps) for the tiles of `tile` rows with rows among entries e0 .. e1-1, in order.
+template <typename Of, typename F>
+__device__ __forceinline__ void each_tile(const AttnArgs &a, int tile, int e0, int e1, Of sizes, F f) {
+    for (int e = e0; e < e1;) {
+        const int r = a.tiles.of(e), next = min((r + 1) * a.tiles.d, e1);
+        const Sizes z = sizes(r);
+        const int rows = z.n * a.group.d, last = min(next, r * a.tiles.d + (rows + tile - 1) / tile);
+        for (; e < last; ++e) f(tile_of(a, z, (e - r * a.tiles.d) * tile, tile).steps);
+        e = next;
+    }
+}
+template <typename Of>
+__device__ __forceinline__ Plan plan_of(const AttnArgs &a, int tile, int entries, Of sizes) {
     const int lane = threadIdx.x & 63;
     auto plus = [](int x, int y) { return x + y; };
-    auto in_front = [&](int x) {
-        int upto = x;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += u;
-        }
-        return upto - x;
-    };
     Plan p;
     p.per = (entries + 63) / 64;
     const int e0 = min(lane * p.per, entries), e1 = min(e0 + p.per, entries);
     int some = 0, most = 0;
-    for (int e = e0; e < e1; ++e) {
-        const int s = entry(e).steps;
-        some += s > 0;
+    each_tile(a, tile, e0, e1, sizes, [&](int s) {
+        ++some;
         most = max(most, s);
-    }
-    p.rank = in_front(some);
+    });
+    p.rank = upto_lane(some) - some;
     const int groups = lanes_reduce<64>(some, plus) * a.H, whole_entries = groups / a.slots * a.slots / a.H;
     most = lanes_reduce<64>(most, [](int x, int y) { return max(x, y); });
     p.whole = whole_entries * a.H;
-    int rest = 0;
-    for (int e = e0, r = p.rank; e < e1; ++e) {
-        const int s = entry(e).steps;
-        if (s > 0 && r++ >= whole_entries) rest += s;
-    }
+    int rest = 0, r = p.rank;
+    each_tile(a, tile, e0, e1, sizes, [&](int s) { rest += r++ >= whole_entries ? s : 0; });
     const float fair = (float)lanes_reduce<64>(rest, plus) * (float)a.H / (float)a.slots;
     // the size that gets through soonest: rounds of pieces, each of which costs about four steps more (not cut: one round of the longest)
     p.piece = 0x2000000;                                           // (more than the steps of 2^31 keys)
+    int size[3], n[3] = {};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) size[k] = max((int)__builtin_ceilf(fair / (float)(k + 1)), 4);
+    r = p.rank;
+    each_tile(a, tile, e0, e1, sizes, [&](int s) {
+        if (r++ < whole_entries) return;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) n[k] += pieces_in(s, size[k]);
+    });
     float best = (float)most;
 #pragma unroll
-    for (int k = 1; k <= 3; ++k) {
-        const int size = max((int)__builtin_ceilf(fair / (float)k), 4);
-        int n = 0;
-        for (int e = e0, r = p.rank; e < e1; ++e) {
-            const int s = entry(e).steps;
-            if (s > 0 && r++ >= whole_entries) n += pieces_in(s, size);
-        }
-        n = lanes_reduce<64>(n, plus) * a.H;
-        const float cost = (float)((n + a.slots - 1) / a.slots * (size + 4));
-        if (n <= kMostPieces && cost < best) {
+    for (int k = 0; k < 3; ++k) {
+        const int all = lanes_reduce<64>(n[k], plus) * a.H;
+        const float cost = (float)((all + a.slots - 1) / a.slots * (size[k] + 4));
+        if (all <= kMostPieces && cost < best) {
             best = cost;
-            p.piece = size;
+            p.piece = size[k];
         }
     }
     p.mine = 0;
-    for (int e = e0, r = p.rank; e < e1; ++e) {
-        const int s = entry(e).steps;
-        if (s > 0) p.mine += r++ >= whole_entries ? pieces_in(s, p.piece) : 1;
-    }
-    p.before = in_front(p.mine);
+    r = p.rank;
+    each_tile(a, tile, e0, e1, sizes, [&](int s) { p.mine += r++ >= whole_entries ? pieces_in(s, p.piece) : 1; });
+    p.before = upto_lane(p.mine) - p.mine;
     p.items = lanes_reduce<64>(p.mine, plus) * a.H;
     return p;
 }
 struct Item { int entry, head, at, pieces; };
-template <typename Entry>
-__device__ __forceinline__ Item item_of(const AttnArgs &a, const Plan &p, int entries, int item, Entry entry) {
+template <typename Of>
+__device__ __forceinline__ Item item_of(const AttnArgs &a, const Plan &p, int tile, int entries, int item, Of sizes) {
     const int lane = threadIdx.x & 63, owner = __builtin_ctzll(__ballot(item < (p.before + p.mine) * a.H));
-    int before = __builtin_amdgcn_readlane(p.before, owner), rank = __builtin_amdgcn_readlane(p.rank, owner), e = owner * p.per, n = 1;
-    for (; e < entries; ++e) {
-        const int s = entry(e).steps;
-        if (s == 0) continue;
-        n = rank++ * a.H >= p.whole ? pieces_in(s, p.piece) : 1;
-        if (item < (before + n) * a.H) break;
-        before += n;
+    int before = __builtin_amdgcn_readlane(p.before, owner), rank = __builtin_amdgcn_readlane(p.rank, owner);
+    const int end = min((owner + 1) * p.per, entries);
+    for (int e0 = owner * p.per;; e0 += 64) {                      // an entry a lane
+        const int e = e0 + lane, r = a.tiles.of(min(e, end - 1));
+        const int steps = e < end ? tile_of(a, sizes(r), a.tiles.rest(e, r) * tile, tile).steps : 0;
+        const unsigned long long some = __ballot(steps > 0);
+        const int nth = rank + __builtin_popcountll(some & ((1ull << lane) - 1));
+        const int n = steps == 0 ? 0 : nth * a.H >= p.whole ? pieces_in(steps, p.piece) : 1, upto = upto_lane(n);
+        const unsigned long long in = __ballot(item < (before + upto) * a.H);
+        if (in || e0 + 64 >= end) {
+            const int at = in ? __builtin_ctzll(in) : 0;
+            Item i;
+            i.entry = e0 + at;
+            i.pieces = __builtin_amdgcn_readlane(n, at);
+            const int rest = item - (before + __builtin_amdgcn_readlane(upto, at) - i.pieces) * a.H;
+            i.at = a.heads.of(rest);                               // (the heads of a request side by side)
+            i.head = a.heads.rest(rest, i.at);
+            return i;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+        rank += __builtin_popcountll(some);
     }
-    (void)lane;
-    Item i;
-    const int in = item - before * a.H;
-    i.entry = min(e, entries - 1);
-    i.at = a.heads.of(in);                                         // (the heads of a request side by side)
-    i.head = a.heads.rest(in, i.at);
-    i.pieces = n;
-    return i;
+}
+
+// Sizes of the first requests, which the plan and every item go through, kept in LDS.
+constexpr int kKept = 512;
+__device__ __forceinline__ void keep_sizes(const AttnArgs &a, Sizes *kept) {
+    for (int r = threadIdx.x; r < min(a.requests, kKept); r += blockDim.x) kept[r] = sizes_of(a, r);
+    __syncthreads();
 }
 
 // The arguments of the kernel, read again: what is kept of them in scalar registers from one end of the kernel to the other does not
@@ -145,17 +167,14 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
     __shared__ float s_scale[2][2][4];                             // [buffer][of keys, log2 of values][sixteen keys]; of keys: < 0 for none
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hl = lane >> 5, mask = (1 << args.shift) - 1;
     const int entries = args.requests * args.tiles.d;
-    auto entry_of = [](const AttnArgs &a, int e) {
-        const int r = a.tiles.of(e);
-        return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
-    };
-    const Plan plan = plan_of(args, entries, [&](int e) { return entry_of(args, e); });
+    __shared__ Sizes kept[kKept];
+    keep_sizes(args, kept);
+    const Plan plan = plan_of(args, ROWS, entries, [&](int r) { return r < kKept ? kept[r] : sizes_of(args, r); });
     for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
         const AttnArgs a = again();
-        auto entry = [&](int e) { return entry_of(a, e); };
-        const Item it = item_of(a, plan, entries, item, entry);
-        const Tile t = entry(it.entry);
+        const Item it = item_of(a, plan, ROWS, entries, item, [&](int r) { return r < kKept ? kept[r] : sizes_of(a, r); });
         const int r = a.tiles.of(it.entry), h = it.head;
+        const Tile t = tile_of(a, r, a.tiles.rest(it.entry, r) * ROWS, ROWS);
         const int first_step = it.pieces > 1 ? it.at * plan.piece : 0, steps_in = it.pieces > 1 ? min(plan.piece, t.steps - first_step) : t.steps;
         const int base = (t.begin & ~(kStep - 1)) + first_step * kStep, stop = min(base + steps_in * kStep, t.end);
         const int steps = stop > base ? (stop - base + kStep - 1) / kStep : 0;
@@ -432,15 +451,15 @@ template <bool BF16, int D, int NW>
 __global__ __launch_bounds__(1024) void kv8_prompt_join_kernel(AttnArgs a) {
     constexpr int ROWS = 32 * NW, QUADS = NW * (D / 8) * 64;       // fours of features of a row
     const int entries = a.requests * a.tiles.d;
-    auto entry = [&](int e) {
-        const int r = a.tiles.of(e);
-        return tile_of(a, r, a.tiles.rest(e, r) * ROWS, ROWS);
-    };
-    const Plan plan = plan_of(a, entries, entry);
+    __shared__ Sizes kept[kKept];
+    keep_sizes(a, kept);
+    auto sizes = [&](int r) { return r < kKept ? kept[r] : sizes_of(a, r); };
+    const Plan plan = plan_of(a, ROWS, entries, sizes);
     for (int item = plan.whole + blockIdx.x; item < plan.items; item += gridDim.x) {
-        const Item it = item_of(a, plan, entries, item, entry);
+        const Item it = item_of(a, plan, ROWS, entries, item, sizes);
         if (it.pieces <= 1) continue;
-        const Tile t = entry(it.entry);
+        const int r = a.tiles.of(it.entry);
+        const Tile t = tile_of(a, r, a.tiles.rest(it.entry, r) * ROWS, ROWS);
         const size_t slot0 = item - plan.whole - it.at * a.H;      // of the group's first piece; the others are H further each
         const int share = ((QUADS + it.pieces - 1) / it.pieces + 63) / 64 * 64;
         for (int i = it.at * share + threadIdx.x; i < min((it.at + 1) * share, QUADS); i += 1024) {
