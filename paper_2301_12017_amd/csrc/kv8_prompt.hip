@@ -85,7 +85,8 @@ __device__ __forceinline__ Plan plan_of(const AttnArgs &a, int tile, int entries
     int rest = 0, r = p.rank;
     each_tile(a, tile, e0, e1, sizes, [&](int s) { rest += r++ >= whole_entries ? s : 0; });
     const float fair = (float)lanes_reduce<64>(rest, plus) * (float)a.H / (float)a.slots;
-    // the size that gets through soonest: rounds of pieces, each of which costs about four steps more (not cut: one round of the longest)
+    // the size that gets through soonest: rounds of pieces, each of which costs about four steps more, and a hundredth of one to join (not
+    // cut: one round of the longest)
     p.piece = 0x2000000;                                           // (more than the steps of 2^31 keys)
     int size[3], n[3] = {};
 #pragma unroll
@@ -100,7 +101,7 @@ __device__ __forceinline__ Plan plan_of(const AttnArgs &a, int tile, int entries
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         const int all = lanes_reduce<64>(n[k], plus) * a.H;
-        const float cost = (float)((all + a.slots - 1) / a.slots * (size[k] + 4));
+        const float cost = (float)((all + a.slots - 1) / a.slots * (size[k] + 4)) + 1.0f + 0.01f * (float)all;
         if (all <= kMostPieces && cost < best) {
             best = cost;
             p.piece = size[k];
