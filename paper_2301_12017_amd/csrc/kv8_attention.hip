@@ -29,6 +29,8 @@
 // launch, the table's words, two steps of a wave one after the other and the sum over its eight waves.
 #include "kv8_attention.hpp"
 
+#include <algorithm>
+
 namespace w4a4 {
 
 int kv8_cache_check(const w4a4_kv8_cache *C);
@@ -457,23 +459,25 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
     }
 }
 
-// How a call is shared out.
+// How the requests of few rows are shared out, and whether there may be requests of many (kv8_prompt.hip).
 struct Split {
-    int nr, tiles;                                                 // nr: 0 for many rows (kv8_prompt.hip)
+    bool some, many;                                               // launched: this kernel; the one for many rows
+    int nr, tiles;
     bool cut;                                                      // groups are cut where they are long
     int places;                                                    // for pieces in the workspace
 };
 Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     Split s;
-    if (kv8_prompt_wanted(C, Q)) return Split{0, kv8_prompt_tiles(C, Q), false, 0};
-    const long rows = (long)Q.queries * (Q.heads / C.heads);
+    s.many = kv8_prompt_wanted(C, Q);
+    s.some = !s.many || Q.requests >= kMixed;
+    const long all = (long)Q.queries * (Q.heads / C.heads), rows = s.many ? kFewRows : all;
     s.nr = rows > 16 && C.features <= 128 ? 2 : 1;
     s.tiles = (int)((rows + 16 * s.nr - 1) / (16 * s.nr));
-    const long keys = Q.window ? min((long)Q.context, (long)Q.window + 16 * s.nr + kStep) : Q.context;
+    const long keys = Q.window ? std::min((long)Q.context, (long)Q.window + 16 * s.nr + kStep) : Q.context;
     const long groups = (long)s.tiles * C.heads * Q.requests;
     // Finding the pieces and joining them costs 4 us, a round of eight steps of a group 2 us.  us whole | cut, 8 key heads of 128: one
     // request of 1024 keys 11.2 | 13.0, 1280 12.6 | 13.0, 2048 16.4 | 13.0; eight of 1280 13.5 | 15.2, 2048 18.0 | 17.2; forty of 1280 30.5 | 29.3.
-    s.cut = keys > 20 * kStep && groups <= kMostGroups;
+    s.cut = s.some && keys > 20 * kStep && groups <= kMostGroups;
     s.places = s.cut ? (int)groups + kSlots : 0;
     return s;
 }
@@ -525,8 +529,10 @@ using namespace w4a4;
 extern "C" size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q) {
     if (check(C, Q) || !Q->tokens || !Q->requests || !Q->queries) return 0;
     const Split s = split_of(*C, *Q);
-    if (!s.nr) return kCounters * sizeof(int) + kv8_prompt_workspace_bytes(*C, *Q);
-    return s.cut ? kCounters * sizeof(int) + (size_t)s.places * 16 * s.nr * (C->features + 2) * sizeof(float) : 0;
+    // (the two kernels come one after the other, and leave their parts in the same place)
+    const size_t few = s.cut ? (size_t)s.places * 16 * s.nr * (C->features + 2) * sizeof(float) : 0;
+    const size_t parts = std::max(few, s.many ? kv8_prompt_workspace_bytes(*C, *Q) : 0);
+    return parts ? kCounters * sizeof(int) + parts : 0;
 }
 
 extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void *out, float *lse, void *workspace,
@@ -537,9 +543,9 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     if (!aligned16(Q->q) || !aligned16(out)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const Split s = split_of(*C, *Q);
     // steps are counted in 32 bits, and divisions (Div) are exact below 2^32
-    const int group = Q->heads / C->heads;
-    if (Q->requests > 65535 || (double)Q->queries * group * group > 4e9 || (double)Q->requests * s.tiles * max(s.tiles, C->heads * C->heads) > 4e9 ||
-        ((double)Q->width * C->block / kStep + 2) * C->heads * s.tiles * Q->requests > 2e9) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const int group = Q->heads / C->heads, tiles = max(s.tiles, s.many ? kv8_prompt_tiles(*C, *Q) : 0);
+    if (Q->requests > 65535 || (double)Q->queries * group * group > 4e9 || (double)Q->requests * tiles * max(tiles, C->heads * C->heads) > 4e9 ||
+        ((double)Q->width * C->block / kStep + 2) * C->heads * tiles * Q->requests > 2e9) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const size_t need = w4a4_kv8_attention_workspace_bytes(C, Q);
     if (need && (!workspace || workspace_bytes < need)) return W4A4_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return W4A4_ERR_UNSUPPORTED_SHAPE;
@@ -547,9 +553,9 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     float *po = reinterpret_cast<float *>(arrived + (need ? kCounters : 0));
     AttnArgs a{static_cast<const uint16_t *>(Q->q), C->k, C->v, C->k_scale, C->v_scale, Q->table, Q->lens, Q->start,
                static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
-               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, 0x7fffffff, Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
+               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, s.many ? kFewRows : 0x7fffffff,
+               Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
-    if (!s.nr) return kv8_prompt(a, *C, *Q, po, st);
     auto run = [&](auto bf16, auto d) {
         constexpr bool BF = decltype(bf16)::value;
         constexpr int D = decltype(d)::value;
@@ -558,10 +564,19 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
         return launch<BF, D, 1>(a, s, st);
     };
     auto typed = [&](auto d) { return Q->dtype == W4A4_BF16 ? run(std::true_type{}, d) : run(std::false_type{}, d); };
-    switch (C->features) {
-        case 64: return typed(std::integral_constant<int, 64>{});
-        case 96: return typed(std::integral_constant<int, 96>{});
-        case 128: return typed(std::integral_constant<int, 128>{});
-        default: return typed(std::integral_constant<int, 256>{});
-    }
+    auto few = [&] {
+        switch (C->features) {
+            case 64: return typed(std::integral_constant<int, 64>{});
+            case 96: return typed(std::integral_constant<int, 96>{});
+            case 128: return typed(std::integral_constant<int, 128>{});
+            default: return typed(std::integral_constant<int, 256>{});
+        }
+    };
+    if (s.some)
+        if (const int rc = few()) return rc;
+    if (!s.many) return W4A4_OK;
+    a.least = s.some ? kFewRows + 1 : 0;
+    a.most = 0x7fffffff;
+    a.tiles = Div(kv8_prompt_tiles(*C, *Q));
+    return kv8_prompt(a, *C, *Q, po, st);
 }

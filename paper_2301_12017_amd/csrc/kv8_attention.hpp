@@ -7,6 +7,8 @@ namespace w4a4 {
 constexpr int kStep = 64;                                          // keys of a step
 constexpr int kSlots = 512, kMostGroups = 4096;                    // pieces of few groups, and groups that are cut, at most
 constexpr int kCounters = kSlots + kMostGroups;                    // in the workspace
+constexpr int kFewRows = 32;                                       // rows of a request and head that kv8_attention.hip takes
+constexpr int kMixed = 4;                                          // requests from which on a call of more rows may have some of few
 constexpr float kUnset = 1.2676506e30f;                            // 2^100: c before a scale of values has been seen
 
 // n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).
@@ -37,7 +39,8 @@ struct AttnArgs {
 struct Sizes { int n, len; };
 __device__ __forceinline__ Sizes sizes_of(const AttnArgs &a, int r) {
     const int n = max(min(min(a.start[r + 1], a.tokens) - max(a.start[r], 0), a.queries), 0), rows = n * a.group.d;
-    return Sizes{rows >= a.least && rows <= a.most ? n : 0, min(max(a.lens[r], 0), (int)min((long)a.width << a.shift, 0x7fffff00L))};
+    const long room = (long)a.width << a.shift;
+    return Sizes{rows >= a.least && rows <= a.most ? n : 0, min(max(a.lens[r], 0), room < 0x7fffff00L ? (int)room : 0x7fffff00)};
 }
 // The rows of a group and the keys they see.
 struct Tile {
@@ -94,8 +97,12 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
 }
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // 2^e, -126 <= e <= 127
 
-// s / t, rounded up, for s + t < 2^31 (a step more or less makes no difference to who uses it, but all use the same)
-__device__ __forceinline__ int pieces_in(int steps, int piece) { return (steps + piece - 1) / piece; }
+// Pieces of `piece` steps that `steps` < 2^26 make: at least enough (where steps are millions, one or two more, which are then empty), the same
+// for all who ask.  By a reciprocal: an integer division is 40 instructions.
+__device__ __forceinline__ int pieces_in(int steps, int piece) {
+    const int n = (int)((float)steps * __builtin_amdgcn_rcpf((float)piece)), left = steps - n * piece;
+    return n + (left > 0) + (left > piece) + (left > 2 * piece) + (left > 3 * piece);
+}
 
 // Many rows (kv8_prompt.hip).
 bool kv8_prompt_wanted(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q);

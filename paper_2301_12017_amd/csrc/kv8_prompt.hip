@@ -73,17 +73,21 @@ __device__ __forceinline__ Plan plan_of(const AttnArgs &a, int tile, int entries
     Plan p;
     p.per = (entries + 63) / 64;
     const int e0 = min(lane * p.per, entries), e1 = min(e0 + p.per, entries);
-    int some = 0, most = 0;
+    int some = 0, most = 0, rest = 0;
     each_tile(a, tile, e0, e1, sizes, [&](int s) {
         ++some;
         most = max(most, s);
+        rest += s;
     });
     p.rank = upto_lane(some) - some;
     const int groups = lanes_reduce<64>(some, plus) * a.H, whole_entries = groups / a.slots * a.slots / a.H;
     most = lanes_reduce<64>(most, [](int x, int y) { return max(x, y); });
     p.whole = whole_entries * a.H;
-    int rest = 0, r = p.rank;
-    each_tile(a, tile, e0, e1, sizes, [&](int s) { rest += r++ >= whole_entries ? s : 0; });
+    int r = p.rank;
+    if (whole_entries) {                                           // (wave-uniform)
+        rest = 0;
+        each_tile(a, tile, e0, e1, sizes, [&](int s) { rest += r++ >= whole_entries ? s : 0; });
+    }
     const float fair = (float)lanes_reduce<64>(rest, plus) * (float)a.H / (float)a.slots;
     // the size that gets through soonest: rounds of pieces, each of which costs about four steps more, and a hundredth of one to join (not
     // cut: one round of the longest)
@@ -93,23 +97,22 @@ __device__ __forceinline__ Plan plan_of(const AttnArgs &a, int tile, int entries
     for (int k = 0; k < 3; ++k) size[k] = max((int)__builtin_ceilf(fair / (float)(k + 1)), 4);
     r = p.rank;
     each_tile(a, tile, e0, e1, sizes, [&](int s) {
-        if (r++ < whole_entries) return;
+        const bool is_whole = r++ < whole_entries;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) n[k] += pieces_in(s, size[k]);
+        for (int k = 0; k < 3; ++k) n[k] += is_whole ? 1 : pieces_in(s, size[k]);
     });
+    p.mine = some;
     float best = (float)most;
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        const int all = lanes_reduce<64>(n[k], plus) * a.H;
+        const int all = (lanes_reduce<64>(n[k], plus) - whole_entries) * a.H;
         const float cost = (float)((all + a.slots - 1) / a.slots * (size[k] + 4)) + 1.0f + 0.01f * (float)all;
         if (all <= kMostPieces && cost < best) {
             best = cost;
             p.piece = size[k];
+            p.mine = n[k];
         }
     }
-    p.mine = 0;
-    r = p.rank;
-    each_tile(a, tile, e0, e1, sizes, [&](int s) { p.mine += r++ >= whole_entries ? pieces_in(s, p.piece) : 1; });
     p.before = upto_lane(p.mine) - p.mine;
     p.items = lanes_reduce<64>(p.mine, plus) * a.H;
     return p;
@@ -513,7 +516,7 @@ int launch(AttnArgs &a, hipStream_t st) {
 
 }  // namespace
 
-bool kv8_prompt_wanted(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) { return (long)Q.queries * (Q.heads / C.heads) > 32; }
+bool kv8_prompt_wanted(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) { return (long)Q.queries * (Q.heads / C.heads) > kFewRows; }
 
 int kv8_prompt_tiles(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     const int rows = 32 * waves_of(C, Q);
