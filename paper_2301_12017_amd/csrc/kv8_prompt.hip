@@ -49,7 +49,7 @@ __device__ __forceinline__ int upto_lane(int x) {                  // sum over t
     return x;
 }
 
-// The work of a call: groups 0 .. whole-1 as they are, then the pieces of the others.  Each wave works it out by itself.
+// The work of a call: groups 0 .. whole-1 as they are, then the pieces of the others.  Each wave works it out by itself (in the join one for all).
 struct Plan {
     int per, whole, piece, items;                                  // entries a lane; whole groups; steps of a piece; groups and pieces in all
     int before, rank;                                              // pieces (or groups) and entries with rows in front of this lane's entries
@@ -458,7 +458,14 @@ __global__ __launch_bounds__(1024) void kv8_prompt_join_kernel(AttnArgs a) {
     __shared__ Sizes kept[kKept];
     keep_sizes(a, kept);
     auto sizes = [&](int r) { return r < kKept ? kept[r] : sizes_of(a, r); };
-    const Plan plan = plan_of(a, ROWS, entries, sizes);
+    __shared__ Plan plans[64];                                     // (its sixteen waves would wait for one another at the same long sums)
+    if (threadIdx.x < 64) plans[threadIdx.x] = plan_of(a, ROWS, entries, sizes);
+    __syncthreads();
+    Plan plan = plans[threadIdx.x & 63];
+    plan.per = __builtin_amdgcn_readfirstlane(plan.per);
+    plan.whole = __builtin_amdgcn_readfirstlane(plan.whole);
+    plan.piece = __builtin_amdgcn_readfirstlane(plan.piece);
+    plan.items = __builtin_amdgcn_readfirstlane(plan.items);
     for (int item = plan.whole + blockIdx.x; item < plan.items; item += gridDim.x) {
         const Item it = item_of(a, plan, ROWS, entries, item, sizes);
         if (it.pieces <= 1) continue;
