@@ -462,6 +462,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
 // How the requests of few rows are shared out, and whether there may be requests of many (kv8_prompt.hip).
 struct Split {
     bool some, many;                                               // launched: this kernel; the one for many rows
+    int most;                                                      // rows of a request that this one takes
     int nr, tiles;
     bool cut;                                                      // groups are cut where they are long
     int places;                                                    // for pieces in the workspace
@@ -470,7 +471,10 @@ Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     Split s;
     s.many = kv8_prompt_wanted(C, Q);
     s.some = !s.many || Q.requests >= kMixed;
-    const long all = (long)Q.queries * (Q.heads / C.heads), rows = s.many ? kFewRows : all;
+    // Where requests of many rows may be among others, single tokens are most of the others: one tile of sixteen rows where a token fits.
+    const int group = Q.heads / C.heads;
+    s.most = !s.many ? kFewRows : group <= 16 ? 16 : kFewRows;
+    const long rows = std::min((long)Q.queries * group, (long)s.most);
     s.nr = rows > 16 && C.features <= 128 ? 2 : 1;
     s.tiles = (int)((rows + 16 * s.nr - 1) / (16 * s.nr));
     const long keys = Q.window ? std::min((long)Q.context, (long)Q.window + 16 * s.nr + kStep) : Q.context;
@@ -553,7 +557,7 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     float *po = reinterpret_cast<float *>(arrived + (need ? kCounters : 0));
     AttnArgs a{static_cast<const uint16_t *>(Q->q), C->k, C->v, C->k_scale, C->v_scale, Q->table, Q->lens, Q->start,
                static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
-               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, s.many ? kFewRows : 0x7fffffff,
+               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, s.most,
                Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
     auto run = [&](auto bf16, auto d) {
@@ -575,7 +579,7 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     if (s.some)
         if (const int rc = few()) return rc;
     if (!s.many) return W4A4_OK;
-    a.least = s.some ? kFewRows + 1 : 0;
+    a.least = s.some ? s.most + 1 : 0;
     a.most = 0x7fffffff;
     a.tiles = Div(kv8_prompt_tiles(*C, *Q));
     return kv8_prompt(a, *C, *Q, po, st);

@@ -8,7 +8,10 @@ constexpr int kStep = 64;                                          // keys of a 
 constexpr int kSlots = 512, kMostGroups = 4096;                    // pieces of few groups, and groups that are cut, at most
 constexpr int kCounters = kSlots + kMostGroups;                    // in the workspace
 constexpr int kFewRows = 32;                                       // rows of a request and head that kv8_attention.hip takes
-constexpr int kMixed = 4;                                          // requests from which on a call of more rows may have some of few
+// Requests from which on a call whose bound allows more rows launches both kernels, each for its requests.  us both | only the one for many rows,
+// 8 key heads of 128, groups of 4: 4 requests of 4000 keys, 100 queries and three single ones 50 | 58, all of 300 queries 157 | 152; 64 of
+// 2000, 1500 queries and 63 single ones 160 | 220.
+constexpr int kMixed = 4;
 constexpr float kUnset = 1.2676506e30f;                            // 2^100: c before a scale of values has been seen
 
 // n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).

@@ -478,6 +478,18 @@ def test_kv8_attention_of_values_with_very_different_scales(B, n):
         assert torch.all((out[:, 0] - p @ V).abs() <= tol)
 
 
+@pytest.mark.parametrize("group, D, dtype", [(1, 64, "fp16"), (4, 128, "bf16"), (8, 96, "fp16"), (20, 64, "bf16"), (5, 256, "fp16")])
+@pytest.mark.parametrize("n, lens, window", [([1, 40, 0, 3, 100, 1, 9], [700, 40, 0, 2900, 300, 1, 1500], 0), ([60, 1, 2, 1, 33], [75, 3000, 2, 640, 2000], 0),
+                                             ([50, 1, 17, 16, 4], [1700, 1, 900, 2100, 64], 130)])
+def test_kv8_attention_of_prompts_and_single_tokens_together(B, n, lens, window, group, D, dtype):
+    _attention_case(B, n, lens, 2, group, D, 32, window, dtype, seed=len(n) + group)
+
+
+def test_kv8_attention_of_more_requests_than_are_kept(B):
+    n = [1 + (40 if i % 97 == 5 else 0) for i in range(700)]
+    _attention_case(B, n, [k + (37 * i) % 90 for i, k in enumerate(n)], 1, 2, 64, 16, 0, "bf16", seed=3)
+
+
 def test_a_row_of_nan_stays_in_its_row(B):
     g = _gen(4)
     cache = _random_cache(B, g, 40, 2, 16, 128)
