@@ -473,7 +473,7 @@ Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
     s.some = !s.many || Q.requests >= kMixed;
     // Where requests of many rows may be among others, single tokens are most of the others: one tile of sixteen rows where a token fits.
     const int group = Q.heads / C.heads;
-    s.most = !s.many ? kFewRows : group <= 16 ? 16 : kFewRows;
+    s.most = !s.many ? kFewRows : group <= 16 ? 16 : group <= 32 ? 32 : kFewRows;
     const long rows = std::min((long)Q.queries * group, (long)s.most);
     s.nr = rows > 16 && C.features <= 128 ? 2 : 1;
     s.tiles = (int)((rows + 16 * s.nr - 1) / (16 * s.nr));

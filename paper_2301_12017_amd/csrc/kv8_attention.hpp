@@ -7,7 +7,9 @@ namespace w4a4 {
 constexpr int kStep = 64;                                          // keys of a step
 constexpr int kSlots = 512, kMostGroups = 4096;                    // pieces of few groups, and groups that are cut, at most
 constexpr int kCounters = kSlots + kMostGroups;                    // in the workspace
-constexpr int kFewRows = 32;                                       // rows of a request and head that kv8_attention.hip takes
+// Rows of a request and head that kv8_attention.hip takes, in tiles that read the keys again.  us there | by kv8_prompt.hip, 8 key heads of 128: 36 or 64
+// rows, 32 requests of 1000 keys 32 | 52, one of 20000 34 | 58, 200 of 1000 208 | 200; 96 rows, 32 of 1000 47 | 54, 8 of 5000 65 | 64, 200 of 1000 310 | 220.
+constexpr int kFewRows = 64;
 // Requests from which on a call whose bound allows more rows launches both kernels, each for its requests.  us both | only the one for many rows,
 // 8 key heads of 128, groups of 4: 4 requests of 4000 keys, 100 queries and three single ones 50 | 58, all of 300 queries 157 | 152; 64 of
 // 2000, 1500 queries and 63 single ones 160 | 220.
