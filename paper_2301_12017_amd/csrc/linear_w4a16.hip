@@ -87,6 +87,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
     u32x4_t x[MT][4];
     const uint16_t *xp[MT];
     bool on[MT];
+    // Rows whose bytes at the same place lie in the same half of a cache line are read in turn, one its first 64 bytes of 128, the next its
+    // second ones: 16 lanes at once would else ask for one half only.  (All rows of a lane are alike: sixteen rows are a multiple of 128 bytes.)
+    // us with | without, N x K: 64 tokens 4096 x 4096 14.9 | 19.2, 16000 x 4096 24.5 | 27.4, 32 tokens 4096 x 4096 8.6 | 11.7, 5 tokens 5.8 | 5.7; the
+    // tiles of 32 tokens and 64 channels have no registers for it (16384 x 4096 19.4 | 18.2).
+    constexpr bool TURNS = !(MT == 2 && NT == 4);
+    const uint32_t half = TURNS && ((uint32_t)((reinterpret_cast<uintptr_t>(a.x) + (size_t)(m0 + col) * a.ldx * 2) >> 6) ^ (uint32_t)col) & 1 ? 32 : 0;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int m = m0 + 16 * t + col;
@@ -157,14 +163,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
             for (int t = 0; t < MT; ++t)
                 if (on[t])
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + 32 * j);
+                    for (int j = 0; j < 4; ++j) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + (32 * j ^ half));
         } else {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     x[t][j] = u32x4_t{0, 0, 0, 0};
-                    if (32 * j < left) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + 32 * j);
+                    const int k = 32 * j ^ half;
+                    if (k < left) x[t][j] = *reinterpret_cast<const u32x4_t *>(xp[t] + 128 * c + k);
                 }
         }
     };
@@ -180,7 +187,16 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xr[i][j] = pair_up(x[i][j]);
+            for (int j = 0; j < 4; j += 2) {
+                u32x4_t v[2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[0][e] = half ? x[i][j + 1][e] : x[i][j][e];
+                    v[1][e] = half ? x[i][j][e] : x[i][j + 1][e];
+                }
+                xr[i][j] = pair_up(v[0]);
+                xr[i][j + 1] = pair_up(v[1]);
+            }
         __builtin_amdgcn_sched_barrier(0);                         // (else their registers are needed twice)
         if (next < c1) load_x(next);
         constexpr int STEPS = 4 / FOLDS;
@@ -284,6 +300,7 @@ int launch(const W4A16Args &a, hipStream_t st) {
 // load instructions as the codes of four tiles; more tiles than that leave CUs without work).  us at one | two | four tiles, N x K:
 //   1 token 16000 x 4096 13.0 | 10.7 | 10.8, 5 tokens 4096 x 4096 5.4 | 6.3 | 9.6, 16 tokens 16000 x 11008 58 | 40 | 32,
 //   32 tokens 16384 x 4096 41 | 25 | 17.6, 20 tokens 4096 x 4096 8.5 | 9.8 | 13.4, 64 tokens 16000 x 4096 71 | 42 | 29.
+// (before rows of x were read in turn, which takes 5 to 30 % off from 12 tokens on, and does not change the order).
 // Four tiles of four times sixteen tokens take the registers of a SIMD for one wave.  Small groups have four sums a chunk, whose
 // operands leave room for one tile (24 tokens 2000 x 8000 in groups of 32: 17 us, two tiles 47), for two where tokens are few.
 template <bool BF16, bool ASYM, bool SMALL, int MT>
