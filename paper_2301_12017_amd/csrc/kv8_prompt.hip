@@ -397,7 +397,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                         for (int i = 0; i < 8; ++i) {
                             const float raw = x[g / 2][8 * (g % 2) + i];
                             float e = __builtin_fmaf(raw, by[g], sh);
-                            if (!PLAIN) e = raw > -INFINITY ? e : -INFINITY;
+                            if (!PLAIN) e = raw == -INFINITY ? raw : e;     // (what the mask took; a NaN stays one)
                             p[i] = __builtin_amdgcn_exp2f(e);
                         }
                         l = __builtin_fmaf(((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])), rv[2 * part + g], l);
