@@ -610,7 +610,8 @@ typedef struct {
  * over its keys in the cache, and the logarithm of the sum of exp(score).  A query that sees nothing (a request of no
  * keys, a row that pads the batch) gets zeros and -infinity.  Rows of tokens that belong to no request are not written.
  * `queries` must hold (of a request that has more, nothing is promised but which rows are written: at most its own); keys past `context` only cost time.  A table entry that names no block
- * of the cache hides its keys.  The workspace (16-byte aligned): its first 18432 bytes are zeros before its first use, and every call leaves
+ * of the cache hides its keys.  A block whose scale is no finite number makes NaN of the rows that see one of its keys, output and
+ * logarithm, and of no others.  The workspace (16-byte aligned): its first 18432 bytes are zeros before its first use, and every call leaves
  * them so; it belongs to one call at a time, any that it is large enough for. */
 size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q);
 int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void *out, float *lse, void *workspace,

@@ -197,8 +197,10 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
         }
         const size_t unit = (size_t)d.v * a.H + h;
         const float kx = a.k_scale[unit], vx = a.v_scale[unit];    // (of keys that are not there: whatever they hold)
-        ksn = d.ok ? kx : 0.0f;
-        vsn = d.ok ? vx : 0.0f;
+        // (a scale that is no finite number makes NaN of the scores, which the mask keeps from rows that do not see them)
+        const bool finite = fabsf(vx) < INFINITY && fabsf(kx) < INFINITY;
+        ksn = d.ok ? finite ? kx : NAN : 0.0f;
+        vsn = d.ok && finite ? vx : 0.0f;
     };
     auto fetch_v = [&](const Blocks &d, int s) {
         const int key = base + kStep * s + 16 * kg;

@@ -168,7 +168,7 @@ template <bool BF16, int D, int NW>
 __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(AttnArgs args) {
     constexpr int ROWS = 32 * NW, THREADS = 64 * NW, FT = D / 32, QS = D / 16, N = (4 * D + THREADS - 1) / THREADS, NH = D <= 128 ? 2 : 1;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[]; // two buffers of [64][keys' row], [D][values' row]
-    __shared__ float s_scale[2][2][4];                             // [buffer][of keys, log2 of values][sixteen keys]; of keys: < 0 for none
+    __shared__ float s_scale[2][2][4];                             // [buffer][of keys, log2 of values][sixteen keys]; of keys: -infinity for none
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hl = lane >> 5, mask = (1 << args.shift) - 1;
     const int entries = args.requests * args.tiles.d;
     __shared__ Sizes kept[kKept];
@@ -228,8 +228,9 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         auto put = [&](int buf) {
             uint16_t *kd = lds + buf * (kBuffer<D> / 2), *vd = kd + kStep * kPitchK<D>;
             if (tid < 4) {
-                s_scale[buf][0][tid] = there ? ks : -1.0f;
-                s_scale[buf][1][tid] = there && vs > 0.0f ? fmaxf(__builtin_amdgcn_logf(vs), -140.0f) : -300.0f;
+                // (a scale that is no finite number makes NaN of the scores, which the mask keeps from rows that do not see them)
+                s_scale[buf][0][tid] = !there ? -INFINITY : fabsf(vs) < INFINITY && fabsf(ks) < INFINITY ? ks : NAN;
+                s_scale[buf][1][tid] = there && vs > 0.0f && vs < INFINITY ? fmaxf(__builtin_amdgcn_logf(vs), -140.0f) : -300.0f;
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
             for (int g = 0; g < 4; ++g) {
                 kf[g] = s_scale[buf][0][g];
                 ex[g] = s_scale[buf][1][g];
-                shown &= kf[g] >= 0.0f;
+                shown &= kf[g] != -INFINITY;
                 top = fmaxf(top, ex[g]);
             }
             if (__builtin_amdgcn_readfirstlane(top + c > 6.0f)) {  // wave-uniform: c follows the scales of values
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 const int key = key0 + 32 * n + 8 * (i / 4) + 4 * hl + i % 4;
-                                x[n][i] = (key <= hi) & (key >= lo) & (kf[2 * (part + n) + i / 8] >= 0.0f) ? x[n][i] : -INFINITY;
+                                x[n][i] = (key <= hi) & (key >= lo) & (kf[2 * (part + n) + i / 8] != -INFINITY) ? x[n][i] : -INFINITY;
                             }
                     }
                     float by[2 * NH], mx = -INFINITY;
