@@ -16,8 +16,10 @@
 //
 // Queries are brought to fp16 by a power of two per row (largest magnitude in [2^14, 2^15)): exact for fp16 and, but for what is
 // 2^28 below the row's largest, for bf16.  Scores and their sums are fp32.  The weights are rounded to fp16 (half a step of 2^-11
-// each, of the size of the output's own rounding) with v_scale in them; they are held at c * v_scale, c a power of two per
-// wave that keeps the largest product near 2^13, so that weights down to 2^-27 keep all their bits.
+// each, of the size of the output's own rounding) with v_scale in them, v_scale = f 2^e, 1/2 <= f < 1:  e is added to the score (in powers of
+// two), so that the row's maximum is that of the products e^s v_scale, and f comes in at the rounding.  The largest product of a row so
+// becomes 2^13 to 2^14, whatever scales the blocks have that it does not see or gives no weight, and products down to 2^-27 of it keep all
+// their bits.  Sums of weights leave e out again, exactly, sixteen keys at a time.
 //
 // Bound by the bytes of the cache for single tokens.  A (request, tile of rows, key head) is a group; a workgroup takes a group or,
 // where requests are long, a piece of one: every workgroup finds from the lengths by itself how long a piece is and
@@ -36,6 +38,9 @@ namespace w4a4 {
 int kv8_cache_check(const w4a4_kv8_cache *C);
 
 namespace {
+
+constexpr float kTop = 14.0f;                                      // log2 of a row's largest weight times 2^e
+constexpr int kLeast = -80;                                        // least e: 2^(kTop - e) times 2^31 keys stays an fp32 number
 
 // Two floats at the coherence point, past the L2s (each XCD has its own): what workgroups leave for one another.  Release and
 // acquire fences at device scope would write back and invalidate a whole L2 each time (a call of 512 workgroups 208 us instead of 49).
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
     constexpr int NT = D / 16, KW = D / 64, KT = D % 64 != 0;      // feature tiles; 64-feature loads of a key, and one of 32
     constexpr int ROWS = NR * 16, REGS = NR * NT * 4, PART = NW * ROWS;
     constexpr bool AHEAD = D * NR <= 128 || D == 256;              // keys AND values of the next step are fetched during this one
-    extern __shared__ __attribute__((aligned(16))) float smem[];   // [wave][REGS][64], then m, l and 1 / c of [wave][ROWS]
+    extern __shared__ __attribute__((aligned(16))) float smem[];   // [wave][REGS][64], then m and l of [wave][ROWS]
     const int tid = threadIdx.x, wave = tid >> 6;
     const int entries = a.requests * a.tiles.d;
     auto entry = [&](int e) {
@@ -210,7 +215,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
     };
 
     float4_t o[NR][NT];
-    float m[NR], l[NR], c = kUnset;
+    float m[NR], l[NR];                                            // m: where the largest product is 2^kTop
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         m[i] = -INFINITY;
@@ -254,21 +259,9 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
         if (AHEAD && more) fetch_k(then, s + NW);
         if (!AHEAD) fetch_v(now, s);
 
-        // c follows the scales of values
-        if (__any(vs * c > 32768.0f)) {
-            float most = vs;
-            most = over_groups(most, max2);
-            const int e = most < INFINITY ? (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 : 0;
-            const float to = power(min(max(12 - e, -100), 100));
-            const float by = to / c;                               // (nothing has been summed yet where c is unset)
-            c = to;
-#pragma unroll
-            for (int i = 0; i < NR; ++i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e2 = 0; e2 < 4; ++e2) o[i][n][e2] *= by;
-        }
+        // v_scale = f 2^e (0, and what is below 2^-81: e as it would be there, f smaller)
+        const int e0 = max((int)(__builtin_bit_cast(uint32_t, vs) >> 23) - 126, kLeast);
+        const float level = (float)e0, f = __builtin_amdgcn_ldexpf(vs, -e0);
         const bool plain = key0 + kStep - 1 <= all_hi && key0 >= all_lo && __all(ok);
         u32x4_t pw[NR][2];
 #pragma unroll
@@ -278,7 +271,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
 #pragma unroll
             for (int T = 0; T < 4; ++T)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[4 * T + e] = sc[i][T][e] * kf;
+                for (int e = 0; e < 4; ++e) x[4 * T + e] = __builtin_fmaf(sc[i][T][e], kf, level);
             if (!plain) {
                 const int key = key0 + 16 * kg;                    // the lane's keys are key .. key + 15, in order
                 const int first = lo[i] - key;
@@ -289,7 +282,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
             float mx = x[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
-            mx = over_groups(mx, max2);
+            mx = over_groups(mx, max2) - kTop;
             if (__any(mx > m[i])) {
                 const float to = fmaxf(mx, m[i]), by = m[i] > -INFINITY ? __builtin_amdgcn_exp2f(m[i] - to) : 0.0f;
                 m[i] = to;
@@ -299,16 +292,18 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[i][n][e] *= by;
             }
-            const float sub = m[i] > -INFINITY ? m[i] : 0.0f, vf = vs * c;
+            const float sub = m[i] > -INFINITY ? m[i] : 0.0f;
+            float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 x[e] = __builtin_amdgcn_exp2f(x[e] - sub);
-                l[i] += x[e];
+                sum += x[e];
             }
+            l[i] += __builtin_amdgcn_ldexpf(sum, -e0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                pw[i][0][e] = pack_halves(x[2 * e] * vf, x[2 * e + 1] * vf);
-                pw[i][1][e] = pack_halves(x[8 + 2 * e] * vf, x[8 + 2 * e + 1] * vf);
+                pw[i][0][e] = pack_halves(x[2 * e] * f, x[2 * e + 1] * f);
+                pw[i][1][e] = pack_halves(x[8 + 2 * e] * f, x[8 + 2 * e + 1] * f);
             }
         }
 #pragma unroll
@@ -339,7 +334,6 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
         if (kg == 0) {
             ml[wave * ROWS + 16 * i + col] = m[i];
             ml[PART + wave * ROWS + 16 * i + col] = sum;
-            ml[2 * PART + wave * ROWS + 16 * i + col] = 1.0f / c;
         }
     }
     __syncthreads();
@@ -359,7 +353,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
             for (int w = 0; w < NW; ++w) {
                 const float f = by[w] > -INFINITY ? __builtin_amdgcn_exp2f(by[w] - mx) : 0.0f;
                 sum += f * ml[PART + w * ROWS + 16 * i + col];
-                by[w] = f * ml[2 * PART + w * ROWS + 16 * i + col];
+                by[w] = f;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) y[k] += smem[(w * REGS + (i * NT + n) * 4 + k) * 64 + lane] * by[w];
             }
@@ -370,7 +364,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
                 const uint32_t y0 = from_float<BF16>(y[0] * inv) | (uint32_t)from_float<BF16>(y[1] * inv) << 16;
                 const uint32_t y1 = from_float<BF16>(y[2] * inv) | (uint32_t)from_float<BF16>(y[3] * inv) << 16;
                 *reinterpret_cast<u32x2_t *>(a.out + at * D + 16 * n + 4 * kg) = u32x2_t{y0, y1};
-                if (n == 0 && kg == 0 && a.lse) a.lse[at] = sum != 0.0f ? (mx + log2f(sum)) * 0.69314718056f : -INFINITY;
+                if (n == 0 && kg == 0 && a.lse) a.lse[at] = log_sum(mx, sum);
             } else {
                 float *to = a.po + ((size_t)blockIdx.x * ROWS + 16 * i + col) * D + 16 * n + 4 * kg;
                 leave2(to, y[0], y[1]);
@@ -416,7 +410,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_attention_kerne
             ml[ROWS + row] = sum != 0.0f ? 1.0f / sum : 0.0f;
             if (row < rows && a.lse) {
                 const int j = a.group.of(t.row0 + row);
-                a.lse[((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(t.row0 + row, j)] = sum != 0.0f ? (most + log2f(sum)) * 0.69314718056f : -INFINITY;
+                a.lse[((size_t)(t.first + j) * a.H + h) * a.group.d + a.group.rest(t.row0 + row, j)] = log_sum(most, sum);
             }
         }
     }
@@ -491,7 +485,7 @@ Split split_of(const w4a4_kv8_cache &C, const w4a4_kv8_queries &Q) {
 template <bool BF16, int D, int NR, int NW, bool CUT>
 int launch_waves(AttnArgs &a, const Split &s, hipStream_t st) {
     auto kern = kv8_attention_kernel<BF16, D, NR, NW, CUT>;
-    constexpr size_t lds = ((size_t)NW * NR * (D / 16) * 4 * 64 + 3 * NW * NR * 16) * sizeof(float);
+    constexpr size_t lds = ((size_t)NW * NR * (D / 16) * 4 * 64 + 2 * NW * NR * 16) * sizeof(float);
     static KernelState ks;
     const void *fn = reinterpret_cast<const void *>(kern);
     const int cus = prepare_kernel(fn, lds, ks);

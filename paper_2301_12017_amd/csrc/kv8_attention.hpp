@@ -14,7 +14,6 @@ constexpr int kFewRows = 64;
 // 8 key heads of 128, groups of 4: 4 requests of 4000 keys, 100 queries and three single ones 50 | 58, all of 300 queries 157 | 152; 64 of
 // 2000, 1500 queries and 63 single ones 160 | 220.
 constexpr int kMixed = 4;
-constexpr float kUnset = 1.2676506e30f;                            // 2^100: c before a scale of values has been seen
 
 // n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).
 struct Div {
@@ -101,6 +100,12 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
     return __builtin_bit_cast(uint32_t, half2_t{(_Float16)a, (_Float16)b});
 }
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // 2^e, -126 <= e <= 127
+
+// log(2^m * sum).  The exponent of the sum is added to m first, which rounds nothing: the two may be large and of different signs.
+__device__ __forceinline__ float log_sum(float m, float sum) {
+    const float whole = m + (float)__builtin_amdgcn_frexp_expf(sum);
+    return sum != 0.0f ? (whole + log2f(__builtin_amdgcn_frexp_mantf(sum))) * 0.69314718056f : -INFINITY;
+}
 
 // Pieces of `piece` steps that `steps` < 2^26 make: at least enough (where steps are millions, one or two more, which are then empty), the same
 // for all who ask.  By a reciprocal: an integer division is 40 instructions.

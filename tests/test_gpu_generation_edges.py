@@ -1,12 +1,15 @@
 """Token generation on the GPU where it can go wrong: rows of NaN, infinities, scales far apart, sizes at their limits, single rows of wider
 arrays, shared workspaces.  Oracles and tolerances as in test_gpu_generation.py."""
+import math
+
 import pytest
 import torch
 
 from tests.gpu_util import has_gpu
-from tests.test_gpu_generation import B, _gen, _random_cache  # noqa: F401 (B is a fixture)
+from tests.test_gpu_generation import TYPES, U, B, _gen, _random_cache  # noqa: F401 (B is a fixture)
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
+
 
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("n, keys, window", [(40, 40, 0), (100, 100, 0), (3, 3, 0), (40, 600, 17), (3, 600, 17), (300, 330, 0)])
@@ -54,3 +57,50 @@ def test_a_scale_that_is_no_number_reaches_only_rows_that_see_its_block(B, n, ke
         assert torch.isnan(call.out[sees.cuda(), 2:]).all() and torch.isnan(call.lse[sees.cuda(), 2:]).all()
         for got, before in ((call.out, want), (call.lse, sums)):
             assert torch.equal(got[:, :2], before[:, :2]) and torch.equal(got[other], before[other])
+
+
+# Queries, keys, window, features: few rows of a request and head.
+FAR = [(1, 100, 0, 64), (5, 99, 0, 128), (5, 291, 40, 64), (16, 3000, 0, 128), (3, 200, 0, 256)]
+# Scale of one block of values, factor of the others' (0.015 to 0.03), types.
+FAR_SCALES = [(2.0 ** -30, 2.0 ** -60, "fp16"), (2.0 ** -30, 2.0 ** -60, "bf16"), (1.0, 2.0 ** -3, "fp16"), (1.0, 2.0 ** -3, "bf16"), (2.0 ** 9, 2.0 ** -24, "fp16"), (2.0 ** 9, 2.0 ** -24, "bf16"),
+              (2.0 ** 100, 2.0 ** -3, "bf16"), (2.0 ** -70, 2.0 ** -90, "bf16")]
+
+
+@pytest.mark.parametrize("most, others, dtype", FAR_SCALES)
+@pytest.mark.parametrize("n, keys, window, D", FAR)
+def test_values_behind_a_far_larger_scale_keep_their_bits(B, n, keys, window, D, most, others, dtype):
+    """Rows that do not see the block of the largest scale, and rows that give its keys hardly any weight, come out as exactly as they would without it."""
+    H, block, g, t = 2, 16, _gen(n + keys), TYPES[dtype]
+    blocks = -(-keys // block)
+    cache = _random_cache(B, g, blocks, H, block, D)
+    cache.v_scale.mul_(others)
+    far = (keys - 1) // block - (1 if n > 20 else 0)
+    cache.v_scale[far] = most
+    if most >= 1:                                                 # its keys are opposite to the queries: rows that see them look elsewhere
+        cache.k[far] = -60
+        cache.k_scale[far] = 0.02
+    q = (torch.randn((n, 2 * H, D), generator=g) * 0.3 + 1.0).to(t)
+    start, lens = torch.tensor([0, n], dtype=torch.int32), torch.tensor([keys], dtype=torch.int32)
+    out, lse = (x.cpu().double() for x in B.kv8_attention(q.cuda(), cache, torch.arange(blocks, dtype=torch.int32, device="cuda")[None], lens.cuda(), start.cuda(), n, keys,
+                                                          D ** -0.5, window=window, want_lse=True))
+    K = (cache.k.cpu().double() * cache.k_scale.cpu().double()[:, :, None, None]).permute(1, 0, 2, 3).reshape(H, -1, D)[:, :keys]
+    V = (cache.v.cpu().double() * cache.v_scale.cpu().double()[:, :, None, None]).permute(1, 0, 3, 2).reshape(H, -1, D)[:, :keys]
+    vs = cache.v_scale.cpu().double().t().repeat_interleave(block, 1)[:, :keys]
+    at, key = keys - n + torch.arange(n)[:, None], torch.arange(keys)[None]
+    sees = (key <= at) & (key > at - window if window else key >= 0)
+    h, tiny = torch.finfo(t).eps / 2, torch.finfo(t).smallest_normal * torch.finfo(t).eps
+    for head in range(2 * H):
+        x = q[:, head].double() @ K[head // 2].t() * D ** -0.5
+        noise = (q[:, head].double().abs() @ K[head // 2].abs().t() * D ** -0.5).amax(1, keepdim=True)
+        x = torch.where(sees, x, -math.inf)
+        z = torch.logsumexp(x, 1, keepdim=True)
+        p = torch.exp(x - z)
+        y, size = p @ V[head // 2], p @ V[head // 2].abs()
+        # a score: D + 6 roundings of its terms' sum, three of numbers below 2^8 when the exponent of a scale comes in (each half a step of 2^-16 and the log
+        # of 2: 92 U); a weight: that, the exponential and half a step of fp16; sums: a rounding per instruction, under the row's OWN sizes
+        weight = (D + 6) * U * noise + 300 * U + 2.0 ** -22
+        # a product of weight and scale below 2^-27 of the row's largest: half a step of fp16's subnormal numbers, 2^-25 where the largest is 2^13, for each key
+        largest = (p * vs[head // 2]).amax(1, keepdim=True) * 127
+        tol = size * (2.0 ** -11 + 2 * weight + (keys / 32 + 40) * U) + h * y.abs() * (1 + 2.0 ** -10) + tiny + keys * 2.0 ** -38 * largest
+        assert torch.all((out[:, head] - y).abs() <= tol), (head, float(((out[:, head] - y).abs() / tol).max()))
+        assert torch.all((lse[:, head, None] - z).abs() <= weight + (keys / 16 + keys / 32 + 40) * U + 2.0 ** -22 * (1 + z.abs()))
