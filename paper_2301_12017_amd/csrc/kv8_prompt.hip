@@ -7,11 +7,13 @@
 // 8 (i / 4) + 4 (lane / 32) + i % 4; values are stored in LDS in the order in which that makes the weights the operand of the
 // second product.
 //
-// A weight times its block's scale is one exponential: exp2(raw * k + (log2(v_scale) + c) - m), c a power of two per wave that
-// keeps the largest near 2^6; the row's sum is taken from the same numbers, divided by the scale again, once per sixteen
-// keys.  (Weights of a block whose scale is 2^20 below the largest one's begin to lose bits; one that is 2^40 below, or 0, counts in the sum and not in the output.)  The maximum m
-// is let fall behind by up to 2^8 before what has been summed is re-scaled: weights stay below 2^15.  (To look for weights that are too
-// large among the packed ones, and for a maximum only then, took 207 us where this takes 190.)
+// A weight times its block's scale is one exponential: exp2(raw * k + log2(v_scale) - m); the row's sum is taken from the same numbers,
+// divided by the scale again, once per sixteen keys.  The maximum m is that of the row's own products e^s v_scale, so that blocks that a row does
+// not see, or gives no weight, take no bits from it: the largest product becomes 2^6, products down to 2^-20 of it keep all their bits as
+// fp16 numbers.  m is let fall behind by up to 2^8 before what has been summed is re-scaled: weights stay below 2^15.  (To look for weights
+// that are too large among the packed ones, and for a maximum only then, took 207 us where this takes 190.)  Scales are taken relative to
+// z, a power of two near the wave's first one that is not 0 (it follows one that is 2^96 above); a block 2^80 below z, or of scale 0, counts as one
+// 2^80 below.
 //
 // Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a sum, half a
 // maximum and half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
@@ -20,14 +22,19 @@
 // the same time with two waves in a SIMD, and more do not fit its registers.
 //
 // A group is 32 NW rows of a request and key head.  Groups beyond whole rounds of the device's workgroups are cut into pieces,
-// whose unfinished outputs a second kernel joins, each of its workgroups a slice of a group.
+// whose outputs a second kernel joins by their sums, each of its workgroups a slice of a group.
 #include "kv8_attention.hpp"
 
 namespace w4a4 {
 namespace {
 
 constexpr int kMostPieces = 768;                                   // of groups that are cut
+constexpr float kTop = 6.0f;                                       // log2 of a row's largest weight when its maximum is up to date
 constexpr float kLag = 8.0f;                                       // how far a maximum may fall behind, in powers of two
+constexpr float kNone = -300.0f;                                   // log2 of a scale of 0
+// Least log2 of a scale relative to z, and the largest before z follows: 2^(kTop + kLag - kBelow) times 2^31 keys stays an fp32 number, and behind
+// a weight of 2^(kTop - kAbove) in the sum others down to 2^-36 of it count.
+constexpr float kBelow = -80.0f, kAbove = 96.0f;
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float16_t mfma32(u32x4_t a, u32x4_t b, float16_t c) {
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
             if (tid < 4) {
                 // (a scale that is no finite number makes NaN of the scores, which the mask keeps from rows that do not see them)
                 s_scale[buf][0][tid] = !there ? -INFINITY : fabsf(vs) < INFINITY && fabsf(ks) < INFINITY ? ks : NAN;
-                s_scale[buf][1][tid] = there && vs > 0.0f && vs < INFINITY ? fmaxf(__builtin_amdgcn_logf(vs), -140.0f) : -300.0f;
+                s_scale[buf][1][tid] = there && vs > 0.0f && vs < INFINITY ? fmaxf(__builtin_amdgcn_logf(vs), -140.0f) : kNone;
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -283,7 +290,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         float16_t o[FT];
 #pragma unroll
         for (int f = 0; f < FT; ++f) o[f] = float16_t{};
-        float m = -INFINITY, behind = -INFINITY, l = 0.0f, c = 200.0f;          // behind: maximum up to which m is kept
+        float m = -INFINITY, l = 0.0f, z = kNone;                  // (z is the same in all lanes)
 
         __syncthreads();                                           // (the last item's keys have been read)
         if (steps > 0) put(0);
@@ -296,9 +303,9 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
             const int buf = s & 1;
             const uint16_t *kd = lds + buf * (kBuffer<D> / 2) + col * kPitchK<D> + 8 * hl;
             const uint16_t *vd = lds + buf * (kBuffer<D> / 2) + kStep * kPitchK<D> + col * kPitchV<D> + 8 * hl;
-            float kf[4], ex[4], rv[4];                             // of sixteen keys: their scale, log2 of the weights' factor, 1 / factor
+            float kf[4], ex[4], rv[4];                             // of sixteen keys: their scale, log2 of the values' scale over 2^z, 1 / that
             bool shown = true;
-            float top = -300.0f;
+            float top = kNone;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 kf[g] = s_scale[buf][0][g];
@@ -306,17 +313,15 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                 shown &= kf[g] != -INFINITY;
                 top = fmaxf(top, ex[g]);
             }
-            if (__builtin_amdgcn_readfirstlane(top + c > 6.0f)) {  // wave-uniform: c follows the scales of values
-                const float by = __builtin_amdgcn_exp2f(4.0f - __builtin_floorf(top) - c);
-                c = 4.0f - __builtin_floorf(top);
-#pragma unroll
-                for (int f = 0; f < FT; ++f)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[f][i] *= by;
+            if (__builtin_amdgcn_readfirstlane(top > z + kAbove)) {            // wave-uniform, seldom more than once
+                const float to = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, __builtin_floorf(top)))), by = fminf(to - z, -kBelow);
+                z = to;
+                m -= by;
+                l *= __builtin_amdgcn_exp2f(by);
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                ex[g] = fmaxf(ex[g] + c, -34.0f);
+                ex[g] = fmaxf(ex[g] - z, kBelow);
                 rv[g] = __builtin_amdgcn_exp2f(-ex[g]);
             }
             if (s + 1 < steps) {                                   // (the other buffer's step is over for every wave)
@@ -376,13 +381,12 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                         float e = x[g / 2][8 * (g % 2)];
 #pragma unroll
                         for (int i = 1; i < 8; ++i) e = fmaxf(e, x[g / 2][8 * (g % 2) + i]);
-                        mx = fmaxf(mx, PLAIN || e > -INFINITY ? e * by[g] : -INFINITY);
+                        mx = fmaxf(mx, PLAIN || e > -INFINITY ? __builtin_fmaf(e, by[g], ex[2 * part + g]) : -INFINITY);
                     }
-                    mx = both_halves(mx, max2);
-                    if (__any(mx > behind)) {                      // the first steps, seldom later; rows that need it
-                        const float to = mx > behind ? fmaxf(mx, m) : m, a0 = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
+                    mx = both_halves(mx, max2) - kTop;
+                    if (__any(mx > m + kLag)) {                    // the first steps, seldom later; rows that need it
+                        const float to = mx > m + kLag ? mx : m, a0 = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
                         m = to;
-                        behind = to + kLag;
                         l *= a0;
 #pragma unroll
                         for (int f = 0; f < FT; ++f)
@@ -419,25 +423,24 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         }
 
         l = both_halves(l, add2);
-        const AttnArgs z = again();
+        const AttnArgs b = again();
+        const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(z) / l : 0.0f;
         const bool mine = wrow + col < t.rows;
-        const size_t at = ((size_t)(t.first + j) * z.H + h) * z.group.d + z.group.rest(row, j);
+        const size_t at = ((size_t)(t.first + j) * b.H + h) * b.group.d + b.group.rest(row, j);
         if (it.pieces > 1) {                                       // [item][wave][four features][lane]: joined later
             const size_t slot = item - plan.whole;
-            const float down = __builtin_amdgcn_exp2f(-c);
             if (any) {
-                float4_t *po = reinterpret_cast<float4_t *>(z.po + slot * ROWS * D) + wave * (D / 2) * 16 + lane;
+                float4_t *po = reinterpret_cast<float4_t *>(b.po + slot * ROWS * D) + wave * (D / 2) * 16 + lane;
 #pragma unroll
                 for (int f = 0; f < FT; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        po[(4 * f + i) * 64] = float4_t{o[f][4 * i] * down, o[f][4 * i + 1] * down, o[f][4 * i + 2] * down, o[f][4 * i + 3] * down};
-                if (hl == 0) *reinterpret_cast<float2 *>(z.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
+                        po[(4 * f + i) * 64] = float4_t{o[f][4 * i] * inv, o[f][4 * i + 1] * inv, o[f][4 * i + 2] * inv, o[f][4 * i + 3] * inv};
+                if (hl == 0) *reinterpret_cast<float2 *>(b.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
             }
             continue;
         }
-        const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(-c) / l : 0.0f;
-        uint16_t *dst = z.out + at * D;
+        uint16_t *dst = b.out + at * D;
 #pragma unroll
         for (int f = 0; f < FT; ++f)
 #pragma unroll
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                 const auto s1 = __builtin_amdgcn_permlane32_swap(two(4 * i + 2), two(4 * i + 6), false, false);
                 if (any && mine) *reinterpret_cast<u32x4_t *>(dst + 32 * f + 8 * (i + hl)) = u32x4_t{(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
             }
-        if (any && mine && hl == 0 && z.lse) z.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+        if (any && mine && hl == 0 && b.lse) b.lse[at] = log_sum(m, l);
     }
 }
 
@@ -486,9 +489,10 @@ __global__ __launch_bounds__(1024) void kv8_prompt_join_kernel(AttnArgs a) {
                 const float2 ml = *reinterpret_cast<const float2 *>(a.pml + (slot * ROWS + in) * 2);
                 const float4_t v = reinterpret_cast<const float4_t *>(a.po + slot * ROWS * D)[i];
                 const float by = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.0f;
-                l += by * ml.y;
+                const float weight = by * ml.y;                    // (of what the piece has for itself: its output is finished)
+                l += weight;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] += by * v[e];
+                for (int e = 0; e < 4; ++e) y[e] += weight * v[e];
             }
             const float inv = l != 0.0f ? 1.0f / l : 0.0f;
             const int j = a.group.of(row), d = 32 * (k / 4) + 8 * (k % 4) + 4 * (lane >> 5);
@@ -496,7 +500,7 @@ __global__ __launch_bounds__(1024) void kv8_prompt_join_kernel(AttnArgs a) {
             const uint32_t y0 = from_float<BF16>(y[0] * inv) | (uint32_t)from_float<BF16>(y[1] * inv) << 16;
             const uint32_t y1 = from_float<BF16>(y[2] * inv) | (uint32_t)from_float<BF16>(y[3] * inv) << 16;
             *reinterpret_cast<u32x2_t *>(a.out + at * D + d) = u32x2_t{y0, y1};
-            if (d == 0 && a.lse) a.lse[at] = l != 0.0f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+            if (d == 0 && a.lse) a.lse[at] = log_sum(m, l);
         }
     }
 }

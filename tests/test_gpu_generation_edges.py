@@ -59,17 +59,16 @@ def test_a_scale_that_is_no_number_reaches_only_rows_that_see_its_block(B, n, ke
             assert torch.equal(got[:, :2], before[:, :2]) and torch.equal(got[other], before[other])
 
 
-# Queries, keys, window, features: few rows of a request and head.
-FAR = [(1, 100, 0, 64), (5, 99, 0, 128), (5, 291, 40, 64), (16, 3000, 0, 128), (3, 200, 0, 256)]
+# Queries, keys, window, features: few rows of a request and head, many.
+FAR_FEW = [(1, 100, 0, 64), (5, 99, 0, 128), (5, 291, 40, 64), (16, 3000, 0, 128), (3, 200, 0, 256)]
+FAR_MANY = [(40, 100, 0, 64), (70, 130, 0, 128), (300, 900, 0, 128), (40, 600, 17, 96), (100, 300, 0, 256), (40, 20000, 0, 64)]
 # Scale of one block of values, factor of the others' (0.015 to 0.03), types.
 FAR_SCALES = [(2.0 ** -30, 2.0 ** -60, "fp16"), (2.0 ** -30, 2.0 ** -60, "bf16"), (1.0, 2.0 ** -3, "fp16"), (1.0, 2.0 ** -3, "bf16"), (2.0 ** 9, 2.0 ** -24, "fp16"), (2.0 ** 9, 2.0 ** -24, "bf16"),
               (2.0 ** 100, 2.0 ** -3, "bf16"), (2.0 ** -70, 2.0 ** -90, "bf16")]
 
 
-@pytest.mark.parametrize("most, others, dtype", FAR_SCALES)
-@pytest.mark.parametrize("n, keys, window, D", FAR)
-def test_values_behind_a_far_larger_scale_keep_their_bits(B, n, keys, window, D, most, others, dtype):
-    """Rows that do not see the block of the largest scale, and rows that give its keys hardly any weight, come out as exactly as they would without it."""
+def _far_case(B, n, keys, window, D, most, others, dtype, kept):
+    """kept: log2 of the products, relative to a row's largest, below which weights lose bits."""
     H, block, g, t = 2, 16, _gen(n + keys), TYPES[dtype]
     blocks = -(-keys // block)
     cache = _random_cache(B, g, blocks, H, block, D)
@@ -99,8 +98,21 @@ def test_values_behind_a_far_larger_scale_keep_their_bits(B, n, keys, window, D,
         # a score: D + 6 roundings of its terms' sum, three of numbers below 2^8 when the exponent of a scale comes in (each half a step of 2^-16 and the log
         # of 2: 92 U); a weight: that, the exponential and half a step of fp16; sums: a rounding per instruction, under the row's OWN sizes
         weight = (D + 6) * U * noise + 300 * U + 2.0 ** -22
-        # a product of weight and scale below 2^-27 of the row's largest: half a step of fp16's subnormal numbers, 2^-25 where the largest is 2^13, for each key
+        # a product of weight and scale below 2^kept of the row's largest: half a step of fp16's subnormal numbers (2^-11 of the smallest normal one) for each key
         largest = (p * vs[head // 2]).amax(1, keepdim=True) * 127
-        tol = size * (2.0 ** -11 + 2 * weight + (keys / 32 + 40) * U) + h * y.abs() * (1 + 2.0 ** -10) + tiny + keys * 2.0 ** -38 * largest
+        tol = size * (2.0 ** -11 + 2 * weight + (keys / 32 + 40) * U) + h * y.abs() * (1 + 2.0 ** -10) + tiny + keys * 2.0 ** (kept - 11) * largest
         assert torch.all((out[:, head] - y).abs() <= tol), (head, float(((out[:, head] - y).abs() / tol).max()))
         assert torch.all((lse[:, head, None] - z).abs() <= weight + (keys / 16 + keys / 32 + 40) * U + 2.0 ** -22 * (1 + z.abs()))
+
+
+@pytest.mark.parametrize("most, others, dtype", FAR_SCALES)
+@pytest.mark.parametrize("n, keys, window, D", FAR_FEW)
+def test_values_behind_a_far_larger_scale_keep_their_bits(B, n, keys, window, D, most, others, dtype):
+    """Rows that do not see the block of the largest scale, and rows that give its keys hardly any weight, come out as exactly as they would without it."""
+    _far_case(B, n, keys, window, D, most, others, dtype, -27)
+
+
+@pytest.mark.parametrize("most, others, dtype", [(min(most, 2.0 ** 80), others, dtype) for most, others, dtype in FAR_SCALES])
+@pytest.mark.parametrize("n, keys, window, D", FAR_MANY)
+def test_values_behind_a_far_larger_scale_keep_their_bits_in_prompts(B, n, keys, window, D, most, others, dtype):
+    _far_case(B, n, keys, window, D, most, others, dtype, -20)
