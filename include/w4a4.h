@@ -545,7 +545,8 @@ typedef enum { W4A4_F16 = 0, W4A4_BF16 = 1 } w4a4_dtype;
 /* out[M,N] = act(X[M,K] * deq(W)^T + bias[N]); X, bias and out in `dtype`, sums in fp32, no rounding in between.
  * X [M, ldx] (ldx elements, a multiple of 8), W canonical codes of either mode, one scale per channel or per group of a multiple
  * of 32 codes (rowsum_deq and esum are not read), bias may be NULL, out dense; pointers 16-byte aligned.  Meant for up to 64
- * tokens (W is read again for every 64, and for every 32 in groups that are no multiple of 128).  act: w4a4_act_fn, GELU on the fp32 value. */
+ * tokens (W is read again for every 64, and for every 32 in groups that are no multiple of 128).  act: w4a4_act_fn, GELU on the fp32 value.
+ * Infinities and NaN in X come out as the sum of products has them (an infinity times a weight of 0 is NaN), in their rows alone. */
 int w4a4_linear_w4a16(const void *X, int dtype, int M, int K, int ldx, const w4a4_weight *W, const void *bias, int act,
                       void *out, void *stream);
 

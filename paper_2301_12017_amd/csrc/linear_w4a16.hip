@@ -57,6 +57,29 @@ __device__ __forceinline__ u32x4_t codes8(uint32_t w) {
     return u32x4_t{(w & 0x000F000Fu) | kOr, ((w >> 4) & 0x000F000Fu) | kOr, ((w >> 8) & 0x000F000Fu) | kOr, ((w >> 12) & 0x000F000Fu) | kOr};
 }
 
+// One result as the definition has it, code by code.  For sums that are no finite number: an infinity in x would meet its own negative in what takes
+// the offset out of the codes, and a bf16 number past 2^120 passes fp32 with the offset's factor.
+template <bool BF16, bool ASYM>
+__device__ __forceinline__ float code_by_code(const W4A16Args &a, int m, int n) {
+    const uint16_t *x = a.x + (size_t)m * a.ldx;
+    const uint8_t *q = a.q + (size_t)n * (a.K >> 1);
+    const int group = a.group ? a.group : a.K;
+    float y = 0.0f;
+    for (int g = 0; g < a.ng; ++g) {
+        const float scale = a.scale[(size_t)n * a.ng + g], zero = ASYM ? a.zero[(size_t)n * a.ng + g] : 0.0f;
+        for (int k = g * group; k < (g + 1) * group && y == y; k += 8) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(q + (k >> 1));
+            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(x + k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float c = ASYM ? (float)(w >> (4 * j) & 15) : (float)((int)(w << (28 - 4 * j)) >> 28);
+                y = __fmaf_rn(ASYM ? __fmaf_rn(c, scale, zero) : c * scale, to_float<BF16>((uint16_t)(v[j / 2] >> (16 * (j % 2)))), y);
+            }
+        }
+    }
+    return y;
+}
+
 struct __attribute__((packed, aligned(4))) Floats4 { float v[4]; };   // (rows of scales begin at any float)
 
 // SMALL: groups that are not a multiple of 128 codes.
@@ -279,6 +302,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
         float y = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
+        if (!(fabsf(y) < INFINITY)) y = code_by_code<BF16, ASYM>(a, m0 + m, n0 + n);
         if (a.bias) y += to_float<BF16>(a.bias[n0 + n]);
         if (a.act == W4A4_ACT_GELU) y = gelu_erf(y);
         a.out[(size_t)(m0 + m) * a.N + n0 + n] = from_float<BF16>(y);

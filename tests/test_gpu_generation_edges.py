@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.gpu_util import has_gpu
-from tests.test_gpu_generation import TYPES, U, B, _gen, _random_cache  # noqa: F401 (B is a fixture)
+from tests.test_gpu_generation import TYPES, U, B, _gen, _random_cache, _weight  # noqa: F401 (B is a fixture)
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
 
@@ -116,3 +116,31 @@ def test_values_behind_a_far_larger_scale_keep_their_bits(B, n, keys, window, D,
 @pytest.mark.parametrize("n, keys, window, D", FAR_MANY)
 def test_values_behind_a_far_larger_scale_keep_their_bits_in_prompts(B, n, keys, window, D, most, others, dtype):
     _far_case(B, n, keys, window, D, most, others, dtype, -20)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,N,K,group,asym", [(7, 264, 512, 128, True), (7, 256, 768, 0, False), (20, 72, 320, 64, True), (40, 136, 384, 128, False), (9, 40, 96, 32, False), (70, 8200, 256, 0, True)])
+def test_linear_w4a16_of_infinities(B, M, N, K, group, asym, dtype):
+    """Infinities of one sign, of both, NaN, and (bf16) numbers that pass fp32 with the offset of the codes: what the definition has, in those rows alone."""
+    g, t = _gen(M + N), TYPES[dtype]
+    W, c, scale, zero = _weight(B, g, N, K, group, asym)
+    X = torch.randn((M, K), generator=g).to(t)
+    inf, nan = float("inf"), float("nan")
+    X[0, 5] = inf
+    X[1, K - 1] = -inf
+    X[2, 3], X[2, K // 2] = inf, -inf
+    X[3, 7] = nan
+    X[4, :9] = inf
+    if dtype == "bf16":
+        X[6, 2], X[6, 40] = 1e37, 3e36
+    got = B.linear_w4a16(X.cuda(), W).cpu().double()
+    w = (c.view(N, -1, group or K) * scale.double()[:, :, None] + (0 if zero is None else zero.double()[:, :, None])).view(N, K)
+    y = torch.stack([(w * x).sum(1) for x in X.double()])         # (0 times an infinity is NaN here)
+    assert bool(torch.isinf(y[:2]).any()) and (asym or bool(torch.isnan(y[:2]).any())) and bool(torch.isnan(y[2]).any()) and bool(torch.isnan(y[3]).all()) and bool(torch.isfinite(y[5:]).all())
+    assert torch.equal(torch.isnan(got), torch.isnan(y)) and torch.equal(got[torch.isinf(y)], y[torch.isinf(y)]) and torch.equal(torch.isinf(got), torch.isinf(y))
+    rows = torch.isfinite(X.double()).all(1)
+    off = 136 if dtype == "bf16" else 8
+    size = X.double()[rows].abs() @ (w.abs() + off * scale.double().amax()).t()
+    h = torch.finfo(t).eps / 2
+    # sums with the codes' offset in them, or one after the other: K + 4 roundings at most
+    assert torch.all((got[rows] - y[rows]).abs() <= h * y[rows].abs() * (1 + 1e-5) + (K + 4) * U * size + 2.0 ** -24)
