@@ -304,7 +304,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
         for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
         if (!(fabsf(y) < INFINITY)) y = code_by_code<BF16, ASYM>(a, m0 + m, n0 + n);
         if (a.bias) y += to_float<BF16>(a.bias[n0 + n]);
-        if (a.act == W4A4_ACT_GELU) y = gelu_erf(y);
+        if (a.act == W4A4_ACT_GELU && y == y) y = gelu_erf(y);     // (which takes a NaN with its sign bit set for a negative number)
         a.out[(size_t)(m0 + m) * a.N + n0 + n] = from_float<BF16>(y);
     }
 }

@@ -144,3 +144,17 @@ def test_linear_w4a16_of_infinities(B, M, N, K, group, asym, dtype):
     h = torch.finfo(t).eps / 2
     # sums with the codes' offset in them, or one after the other: K + 4 roundings at most
     assert torch.all((got[rows] - y[rows]).abs() <= h * y[rows].abs() * (1 + 1e-5) + (K + 4) * U * size + 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_linear_w4a16_gelu_of_nan_of_either_sign(B, dtype):
+    g, t = _gen(1), TYPES[dtype]
+    W, *_ = _weight(B, g, 40, 256, 128, False)
+    X = torch.randn((5, 256), generator=g).to(t)
+    want = B.linear_w4a16(X.cuda(), W, None, B.ACT_GELU)
+    bits = X.view(torch.int16)
+    bits[1, 9], bits[3, 200] = (0x7E00, 0x7E00 - 0x8000) if dtype == "fp16" else (0x7FC0, 0x7FC0 - 0x8000)
+    X[4, 0], X[4, 1] = float("inf"), -float("inf")
+    got = B.linear_w4a16(X.cuda(), W, None, B.ACT_GELU)
+    assert torch.isnan(got[[1, 3]]).all() and torch.equal(got[[0, 2]], want[[0, 2]])
+    assert torch.equal(torch.isnan(got[4]), torch.isnan(B.linear_w4a16(X.cuda(), W)[4]))
