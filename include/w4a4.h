@@ -604,7 +604,7 @@ typedef struct {
     int ldq;                /* elements, a multiple of 8                                       */
     int requests, width;
     int queries, context;   /* upper bounds of a request's queries and keys                    */
-    int window;             /* keys that a query sees, itself included; 0: all before it       */
+    int window;             /* keys that a query sees, itself included; 0, or past 2^30: all before it */
 } w4a4_kv8_queries;
 
 /* out [tokens, heads, features], lse [tokens, heads] (may be NULL): causal attention of each request's queries, its last positions,

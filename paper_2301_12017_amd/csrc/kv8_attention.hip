@@ -549,11 +549,12 @@ extern "C" int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_querie
     const size_t need = w4a4_kv8_attention_workspace_bytes(C, Q);
     if (need && (!workspace || workspace_bytes < need)) return W4A4_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const int window = Q->window > 1 << 30 ? 0 : Q->window;        // (positions minus a window stay above -2^31)
     int *arrived = static_cast<int *>(workspace);
     float *po = reinterpret_cast<float *>(arrived + (need ? kCounters : 0));
     AttnArgs a{static_cast<const uint16_t *>(Q->q), C->k, C->v, C->k_scale, C->v_scale, Q->table, Q->lens, Q->start,
                static_cast<uint16_t *>(out), lse, po, po + (size_t)s.places * 16 * s.nr * C->features, arrived, Q->ldq, Q->tokens, C->blocks, C->heads,
-               __builtin_ctz(C->block), C->blocks ? Q->width : 0, Q->window, Q->queries, Q->requests, 0, 0, s.most,
+               __builtin_ctz(C->block), C->blocks ? Q->width : 0, window, Q->queries, Q->requests, 0, 0, s.most,
                Div(group), Div(s.tiles), Div(C->heads), Q->scale * 1.44269504f};
     hipStream_t st = as_stream(stream);
     auto run = [&](auto bf16, auto d) {

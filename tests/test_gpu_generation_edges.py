@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.gpu_util import has_gpu
-from tests.test_gpu_generation import TYPES, U, B, _gen, _random_cache, _weight  # noqa: F401 (B is a fixture)
+from tests.test_gpu_generation import TYPES, U, B, _attention_case, _gen, _random_cache, _weight  # noqa: F401 (B is a fixture)
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
 
@@ -158,3 +158,10 @@ def test_linear_w4a16_gelu_of_nan_of_either_sign(B, dtype):
     got = B.linear_w4a16(X.cuda(), W, None, B.ACT_GELU)
     assert torch.isnan(got[[1, 3]]).all() and torch.equal(got[[0, 2]], want[[0, 2]])
     assert torch.equal(torch.isnan(got[4]), torch.isnan(B.linear_w4a16(X.cuda(), W)[4]))
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 40, 2 ** 30 + 1, 2 ** 30])
+@pytest.mark.parametrize("n, lens", [([5, 1], [2, 70]), ([70, 9], [50, 9])])
+def test_kv8_attention_with_the_largest_windows(B, n, lens, window):
+    """More queries than keys, so that the first ones stand at negative positions."""
+    _attention_case(B, n, lens, 1, 2, 64, 16, window, "fp16", seed=n[0])
