@@ -561,7 +561,8 @@ int w4a4_linear_w4a16(const void *X, int dtype, int M, int K, int ldx, const w4a
  *   lens_out[r]    lens[r] + new_tokens[r] where served, 0 where ended, else lens[r];  state_out[2]: the state afterwards
  *   start          [requests + 1] sums of the new tokens: request r's are tokens start[r] .. start[r+1]-1 of the step
  *   slots, positions  [tokens] of each new token, in that order: block * (tokens of a block) + place in it, and its place in its
- *                  request; -1 for tokens of requests that are not served and behind the last one.  Tokens past `tokens` are left out.
+ *                  request; -1 for tokens of requests that are not served and behind the last one, and for slots of what no cache can have
+ *                  as a block (negative, or slots past 2^31).  Tokens past `tokens` are left out.
  * table and ring are updated in place (entries that change); state_out and lens_out are other arrays than state and lens, which
  * makes the call repeatable.  block: 16, 32, 64 or 128 tokens.  ring must hold at most `capacity` free blocks in all. */
 int w4a4_kv8_plan(const int32_t *lens, const int32_t *new_tokens, int requests, int32_t *table, int width, int32_t *ring,

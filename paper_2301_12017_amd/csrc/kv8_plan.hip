@@ -172,7 +172,8 @@ __global__ __launch_bounds__(THREADS) void kv8_plan_kernel(PlanArgs a) {
             pos = c_len[lo] + (int)(t - c_start[lo]);
             const int b = pos >> a.shift, have = c_have[lo];
             const int id = b < have ? a.table[(size_t)(c0 + lo) * a.width + b] : a.ring[wrap(head + c_take[lo] + (b - have), a.capacity)];
-            slot = (int)((uint32_t)id << a.shift) + (pos & ((1 << a.shift) - 1));
+            // (what cannot be a block's number makes no slot: shifted out of its word it would be another block's)
+            if ((unsigned)id < 0x80000000u >> a.shift) slot = (id << a.shift) + (pos & ((1 << a.shift) - 1));
         }
         a.slots[t] = slot;
         a.positions[t] = pos;

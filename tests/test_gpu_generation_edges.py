@@ -165,3 +165,17 @@ def test_linear_w4a16_gelu_of_nan_of_either_sign(B, dtype):
 def test_kv8_attention_with_the_largest_windows(B, n, lens, window):
     """More queries than keys, so that the first ones stand at negative positions."""
     _attention_case(B, n, lens, 1, 2, 64, 16, window, "fp16", seed=n[0])
+
+
+@pytest.mark.parametrize("block", [16, 128])
+def test_kv8_plan_makes_no_slot_of_what_is_no_block(B, block):
+    """Entries of a table and of a ring whose number, times the tokens of a block, passes 32 bits."""
+    wild = [2 ** 32 // block + 5, -5, 2 ** 31 - 1, -2 ** 31, 2 ** 31 // block, 2 ** 31 // block - 1, 3]
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    R = len(wild)
+    call = B.kv8_plan(i32([3] * R), i32([2] * R), i32([[w, 9] for w in wild]), i32([7]), i32([0, 0]), block, 2 * R)
+    want = [s for w in wild for s in ([block * w + 3, block * w + 4] if 0 <= w < 2 ** 31 // block else [-1, -1])]
+    assert call.slots.tolist() == want and call.positions.tolist() == [3, 4] * R
+    call = B.kv8_plan(i32([0] * R), i32([1] * R), i32([[9, 9]] * R), i32(wild), i32([0, R]), block, R)
+    assert call.slots.tolist() == [block * w if 0 <= w < 2 ** 31 // block else -1 for w in wild] and call.positions.tolist() == [0] * R
+    assert call.table[:, 0].tolist() == wild
