@@ -839,7 +839,7 @@ class PreparedLinearW4A16(_Prepared):
         assert out.dtype == X.dtype and out.shape == (M, W.N) and out.is_contiguous()
         self.out, self.w = out, W.c()
         self.keep = (X, W, bias)
-        self._lay_out("w4a4_linear_w4a16", (X, self.w, bias, out), (_dtype(X.dtype), M, K, X.stride(0) if M > 1 else max(K, X.stride(0)), act))
+        self._lay_out("w4a4_linear_w4a16", (X, self.w, bias, out), (_dtype(X.dtype), M, K, X.stride(0) if M > 1 else K, act))
 
 
 def linear_w4a16(X: torch.Tensor, W: QWeight, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -902,7 +902,7 @@ def _kv_rows(C: KVCache8, x: torch.Tensor) -> int:
     """Elements between the rows of x [tokens, heads, features]; the heads of a token lie together."""
     assert x.is_cuda and x.dim() == 3 and x.shape[1:] == (C.heads, C.features) and x.stride(2) == 1
     assert C.heads == 1 or x.stride(1) == C.features
-    return max(x.stride(0), C.heads * C.features) if x.shape[0] <= 1 else x.stride(0)
+    return C.heads * C.features if x.shape[0] <= 1 else x.stride(0)           # (of a single row the stride says nothing)
 
 
 class PreparedKV8Append(_Prepared):
@@ -948,7 +948,7 @@ class PreparedKV8Attention(_Prepared):
         R = lens.numel()
         assert q.is_cuda and D == cache.features and q.stride(2) == 1 and (G == 1 or q.stride(1) == D)
         assert table.dim() == 2 and table.shape[0] == R and start.numel() == R + 1
-        ldq = max(q.stride(0), G * D) if T <= 1 else q.stride(0)
+        ldq = G * D if T <= 1 else q.stride(0)
         if out is None:
             out = torch.empty((T, G, D), dtype=q.dtype, device=q.device)
         assert out.dtype == q.dtype and out.shape == (T, G, D) and out.is_contiguous()

@@ -179,3 +179,20 @@ def test_kv8_plan_makes_no_slot_of_what_is_no_block(B, block):
     call = B.kv8_plan(i32([0] * R), i32([1] * R), i32([[9, 9]] * R), i32(wild), i32([0, R]), block, R)
     assert call.slots.tolist() == [block * w if 0 <= w < 2 ** 31 // block else -1 for w in wild] and call.positions.tolist() == [0] * R
     assert call.table[:, 0].tolist() == wild
+
+
+@pytest.mark.parametrize("stride", [1001, 3, 64 * 4])
+def test_single_rows_of_any_stride(B, stride):
+    """One row of a wider array, or of a broadcast one: its stride says nothing."""
+    g = _gen(stride)
+    row = torch.randn((1, 256), generator=g).half().cuda()
+    x = row.as_strided((1, 256), (stride, 1))
+    W, *_ = _weight(B, g, 64, 256, 64, True)
+    assert torch.equal(B.linear_w4a16(x, W), B.linear_w4a16(row.clone(), W))
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    found = []
+    for kv in (row.view(1, 4, 64), row.as_strided((1, 4, 64), (stride, 64, 1))):
+        cache = B.KVCache8.new(2, 4, 64)
+        B.kv8_append(cache, kv, kv, i32(16))
+        found.append((cache.k, cache.v, B.kv8_attention(kv, cache, i32(1)[None], i32(1), i32(0, 1), 1, 1, 0.125)))
+    assert all(torch.equal(a, b) for a, b in zip(*found)) and found[0][0].any()
