@@ -831,12 +831,12 @@ class PreparedLinearW4A16(_Prepared):
     weights in canonical codes.  The result, in the type of X, is in `out`."""
 
     def __init__(self, X: torch.Tensor, W: QWeight, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None):
-        assert X.is_cuda and X.dim() == 2 and X.stride(1) == 1
-        assert bias is None or (bias.dtype == X.dtype and bias.shape == (W.N,) and bias.is_contiguous())
+        assert X.is_cuda and W.q.is_cuda and X.dim() == 2 and X.stride(1) == 1
+        assert bias is None or (bias.is_cuda and bias.dtype == X.dtype and bias.shape == (W.N,) and bias.is_contiguous())
         M, K = X.shape
         if out is None:
             out = torch.empty((M, W.N), dtype=X.dtype, device=X.device)
-        assert out.dtype == X.dtype and out.shape == (M, W.N) and out.is_contiguous()
+        assert out.is_cuda and out.dtype == X.dtype and out.shape == (M, W.N) and out.is_contiguous()
         self.out, self.w = out, W.c()
         self.keep = (X, W, bias)
         self._lay_out("w4a4_linear_w4a16", (X, self.w, bias, out), (_dtype(X.dtype), M, K, X.stride(0) if M > 1 else K, act))
@@ -951,7 +951,7 @@ class PreparedKV8Attention(_Prepared):
         ldq = G * D if T <= 1 else q.stride(0)
         if out is None:
             out = torch.empty((T, G, D), dtype=q.dtype, device=q.device)
-        assert out.dtype == q.dtype and out.shape == (T, G, D) and out.is_contiguous()
+        assert out.is_cuda and out.dtype == q.dtype and out.shape == (T, G, D) and out.is_contiguous()
         self.out, self.lse = out, torch.empty((T, G), dtype=torch.float32, device=q.device) if want_lse else None
         self.c = cache.c()
         self.q = _KV8Queries(_address(q), _address(table), _address(lens), _address(start), scale, _dtype(q.dtype), T, G, ldq, R, table.shape[1],

@@ -196,3 +196,18 @@ def test_single_rows_of_any_stride(B, stride):
         B.kv8_append(cache, kv, kv, i32(16))
         found.append((cache.k, cache.v, B.kv8_attention(kv, cache, i32(1)[None], i32(1), i32(0, 1), 1, 1, 0.125)))
     assert all(torch.equal(a, b) for a, b in zip(*found)) and found[0][0].any()
+
+
+def test_generation_refuses_host_tensors(B):
+    """A result, a bias or weights that are not on the GPU are refused before anything is launched."""
+    g = _gen(1)
+    W, *_ = _weight(B, g, 64, 256, 64, False)
+    x = torch.randn((3, 256), generator=g).half().cuda()
+    host = B.QWeight(W.q.cpu(), W.scale.cpu(), None, None, None, 64, 256, 64, B.SYM)
+    for args in ((x, W, torch.zeros(64, dtype=torch.float16)), (x, W, None, B.ACT_NONE, torch.zeros((3, 64), dtype=torch.float16)), (x, host), (x.cpu(), W)):
+        with pytest.raises(AssertionError):
+            B.PreparedLinearW4A16(*args)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    cache = B.KVCache8.new(2, 4, 64)
+    with pytest.raises(AssertionError):
+        B.PreparedKV8Attention(x.view(3, 4, 64), cache, i32(1)[None], i32(3), i32(0, 3), 3, 3, 0.125, out=torch.zeros((3, 4, 64), dtype=torch.float16))
