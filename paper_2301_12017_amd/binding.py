@@ -937,12 +937,30 @@ def kv8_read(cache: KVCache8, slots: torch.Tensor, dtype=torch.float16):
     return call.k, call.v
 
 
+class KV8Workspace:
+    """Memory for w4a4_kv8_attention calls that come one after the other on one stream, as large as the largest so far needs.  Only its first
+    bytes have to be zeros, once: the calls leave them so."""
+    ZEROS = 18432
+
+    def __init__(self):
+        self.bytes = None
+
+    def of(self, need: int, device) -> Optional[torch.Tensor]:
+        if not need:
+            return None
+        if self.bytes is None or self.bytes.numel() < need or self.bytes.device != device:
+            self.bytes = torch.empty((need,), dtype=torch.uint8, device=device)
+            self.bytes[:self.ZEROS].zero_()
+        return self.bytes
+
+
 class PreparedKV8Attention(_Prepared):
     """A w4a4_kv8_attention call: queries q [tokens, heads, features] over the cache.  `queries` and `context` are upper bounds of a
-    request's queries and keys.  The results are in `out` and, where asked for, `lse`."""
+    request's queries and keys.  The results are in `out` and, where asked for, `lse`.  Calls that follow each other on a stream may
+    share a workspace; else the call has its own."""
 
     def __init__(self, q: torch.Tensor, cache: KVCache8, table: torch.Tensor, lens: torch.Tensor, start: torch.Tensor, queries: int, context: int,
-                 scale: float, window=0, want_lse=False, out: Optional[torch.Tensor] = None):
+                 scale: float, window=0, want_lse=False, out: Optional[torch.Tensor] = None, workspace: Optional[KV8Workspace] = None):
         _i32(table, lens, start)
         T, G, D = q.shape
         R = lens.numel()
@@ -957,14 +975,14 @@ class PreparedKV8Attention(_Prepared):
         self.q = _KV8Queries(_address(q), _address(table), _address(lens), _address(start), scale, _dtype(q.dtype), T, G, ldq, R, table.shape[1],
                              queries, context, window)
         need = int(lib().w4a4_kv8_attention_workspace_bytes(ctypes.byref(self.c), ctypes.byref(self.q)))
-        self.workspace = torch.zeros((need,), dtype=torch.uint8, device=q.device) if need else None
+        self.workspace = (workspace or KV8Workspace()).of(need, q.device)
         self.keep = (q, cache, table, lens, start)
         self._lay_out("w4a4_kv8_attention", (self.c, self.q, self.out, self.lse, self.workspace), n=need)
 
 
-def kv8_attention(q, cache, table, lens, start, queries: int, context: int, scale: float, window=0, want_lse=False):
+def kv8_attention(q, cache, table, lens, start, queries: int, context: int, scale: float, window=0, want_lse=False, workspace: Optional[KV8Workspace] = None):
     """w4a4_kv8_attention: out [tokens, heads, features], or (out, lse)."""
-    call = PreparedKV8Attention(q, cache, table, lens, start, queries, context, scale, window, want_lse)
+    call = PreparedKV8Attention(q, cache, table, lens, start, queries, context, scale, window, want_lse, workspace=workspace)
     call()
     return (call.out, call.lse) if want_lse else call.out
 

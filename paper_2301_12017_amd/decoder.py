@@ -22,6 +22,7 @@ class Books:
         self.table, self.ring = z(requests, -(-context // block)), torch.arange(blocks, dtype=torch.int32, device=device)
         self.lens, self.state = [z(requests), z(requests)], [torch.tensor([0, blocks], dtype=torch.int32, device=device), z(2)]
         self.now = 0                                       # which of the two holds the present
+        self.workspace = B.KV8Workspace()                  # of the layers' attention, one after the other
 
     def plan(self, new_tokens: torch.Tensor, tokens: int) -> B.PreparedKV8Plan:
         """Books `new_tokens` [requests] (negative: the request has ended), `tokens` of them at most."""
@@ -48,7 +49,7 @@ class DecoderLayer:
         T, D = x.shape[0], self.features
         q, k, v = (t.view(T, -1, D) for t in B.linear_w4a16(x, self.qkv, self.bias[0]).split([self.heads * D, self.kv_heads * D, self.kv_heads * D], 1))
         B.kv8_append(self.cache, k, v, plan.slots)
-        a = B.kv8_attention(q, self.cache, books.table, plan.lens, plan.start, queries, books.context, D ** -0.5)
+        a = B.kv8_attention(q, self.cache, books.table, plan.lens, plan.start, queries, books.context, D ** -0.5, workspace=books.workspace)
         x = self._norm(B.linear_w4a16(a.view(T, -1), self.out, self.bias[1]), x, self.ln1)
         h = B.linear_w4a16(x, self.ffn1, self.bias[2], B.ACT_GELU)
         return self._norm(B.linear_w4a16(h, self.ffn2, self.bias[3]), x, self.ln2)

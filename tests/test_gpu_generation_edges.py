@@ -211,3 +211,42 @@ def test_generation_refuses_host_tensors(B):
     cache = B.KVCache8.new(2, 4, 64)
     with pytest.raises(AssertionError):
         B.PreparedKV8Attention(x.view(3, 4, 64), cache, i32(1)[None], i32(3), i32(0, 3), 3, 3, 0.125, out=torch.zeros((3, 4, 64), dtype=torch.float16))
+
+
+def test_one_workspace_for_calls_of_every_shape(B):
+    """Cut requests, batches that mix prompts and single tokens, prompts, smaller and larger in turn: the bits of calls with workspaces of their own."""
+    g, shared = _gen(3), B.KV8Workspace()
+    cache = _random_cache(B, g, 700, 2, 32, 128)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    shapes = [([1], [9000]), ([1, 40, 1, 3, 100], [700, 60, 2900, 300, 4000]), ([1] * 9, [2000] * 9), ([700], [5000]), ([2, 1], [6000, 3]), ([1], [30]), ([400, 90], [3000, 2000])]
+    calls, want = [], []
+    for n, lens in shapes:
+        have = [-(-x // 32) for x in lens]
+        table = torch.zeros((len(n), max(have)), dtype=torch.int32)
+        ids = torch.randperm(700, generator=g).int()
+        for r, h in enumerate(have):
+            table[r, :h] = ids[sum(have[:r]):sum(have[:r + 1])]
+        args = (torch.randn((sum(n), 8, 128), generator=g).half().cuda(), cache, table.cuda(), i32(lens), i32([sum(n[:i]) for i in range(len(n) + 1)]), max(n), max(lens), 0.09)
+        want.append([t.clone() for t in B.kv8_attention(*args, want_lse=True)])
+        calls.append(args)
+    for _ in range(2):
+        for args, w in zip(calls, want):
+            got = B.kv8_attention(*args, want_lse=True, workspace=shared)
+            assert all(torch.equal(a, b) for a, b in zip(got, w))
+    size = shared.bytes.numel()
+    assert size >= 700 * 1024 and not shared.bytes[:shared.ZEROS].any()
+    B.kv8_attention(*calls[0], workspace=shared)
+    assert shared.bytes.numel() == size
+
+
+def test_a_workspace_is_not_filled_with_zeros(B, monkeypatch):
+    """Of the workspace of a prompt, a hundred megabytes, only the counters are."""
+    cache = B.KVCache8.new(20, 8, 128, 32)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    table, q, args = torch.arange(20, dtype=torch.int32, device="cuda")[None], torch.zeros((300, 8, 128), dtype=torch.float16, device="cuda"), (i32(600), i32(0, 300))
+    made, zeros, zero_ = [], torch.zeros, torch.Tensor.zero_
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: (made.append(zeros(*a, **k)), made[-1])[1])
+    monkeypatch.setattr(torch.Tensor, "zero_", lambda t: (made.append(t), zero_(t))[1])
+    call = B.PreparedKV8Attention(q, cache, table, *args, 300, 600, 0.09)
+    call()
+    assert call.workspace.numel() > 10 ** 8 and made and all(t.numel() * t.element_size() <= 18432 for t in made)
