@@ -79,15 +79,18 @@ class Decoder:
         return B.linear_w4a16(x, self.head)[:, :len(self.tokens)]
 
     def generate(self, prompts, new: int) -> torch.Tensor:
-        """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids)."""
+        """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids).  Requests
+        go on from what they hold, and end with the call: their blocks are free again."""
         dev, n = self.tokens.device, [len(p) for p in prompts]
         ids, new_tokens = torch.cat([p.to(dev) for p in prompts]).long(), torch.tensor(n, dtype=torch.int32, device=dev)
         one, queries, found = torch.ones_like(new_tokens), max(n), []
         for _ in range(new):
             x, plan = self.step(ids, new_tokens, queries)
-            ids = self.logits(x[(plan.start[1:] - 1).long()].contiguous()).argmax(1)
+            last = (plan.start[1:] - 1).long()
+            ids = self.logits(x[last].contiguous()).argmax(1)
             found.append(ids)
             new_tokens, queries = one, 1
+        self.step(ids[:0], -one, 1)
         return torch.stack(found, 1)
 
 
@@ -109,7 +112,6 @@ if __name__ == "__main__":
     draw = torch.Generator().manual_seed(1)
     prompts = [torch.randint(0, 32000, (100 + 37 * i,), generator=draw) for i in range(16)]
     decoder.generate(prompts, 2)
-    decoder.step(torch.zeros(0, dtype=torch.long, device="cuda"), torch.full((16,), -1, dtype=torch.int32, device="cuda"), 1)      # (all requests end)
     torch.cuda.synchronize()
     began = time.perf_counter()
     found = decoder.generate(prompts, 64)
