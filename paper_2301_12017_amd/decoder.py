@@ -80,17 +80,24 @@ class Decoder:
 
     def generate(self, prompts, new: int) -> torch.Tensor:
         """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids).  Requests
-        go on from what they hold, and end with the call: their blocks are free again."""
+        go on from what they hold, and end with the call: their blocks are free again.  Raises where a request found no blocks, or
+        no room in its context."""
         dev, n = self.tokens.device, [len(p) for p in prompts]
+        if max(n) + new - 1 > self.books.context:
+            raise ValueError(f"{max(n)} tokens and {new - 1} behind them do not fit a context of {self.books.context}")
         ids, new_tokens = torch.cat([p.to(dev) for p in prompts]).long(), torch.tensor(n, dtype=torch.int32, device=dev)
         one, queries, found = torch.ones_like(new_tokens), max(n), []
+        served = torch.ones((), dtype=torch.bool, device=dev)              # (looked at once, behind the last step: nothing waits for it)
         for _ in range(new):
             x, plan = self.step(ids, new_tokens, queries)
             last = (plan.start[1:] - 1).long()
+            served &= (plan.positions[last] >= 0).all()
             ids = self.logits(x[last].contiguous()).argmax(1)
             found.append(ids)
             new_tokens, queries = one, 1
         self.step(ids[:0], -one, 1)
+        if not served:
+            raise RuntimeError("a request was not served: too few free blocks, or its context was full")
         return torch.stack(found, 1)
 
 

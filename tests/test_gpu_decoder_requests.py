@@ -1,4 +1,4 @@
-"""Decoder.generate: one call after the other."""
+"""Decoder.generate: requests that are not served, one call after the other."""
 import pytest
 import torch
 
@@ -14,6 +14,12 @@ def _decoder(**kw):
     return dec.random_decoder(hidden=256, heads=4, kv_heads=2, ffn=512, requests=3, seed=3, **{"context": 128, **kw})
 
 
+def _fewer_blocks(d, blocks):
+    """The ring of free blocks cut to its first `blocks`."""
+    d.books.state[d.books.now][1] = blocks
+    return d
+
+
 def test_generate_again_begins_anew():
     d = _decoder()
     first, again = d.generate(PROMPTS, 6), d.generate(PROMPTS, 6)
@@ -21,3 +27,21 @@ def test_generate_again_begins_anew():
     assert d.books.lens[d.books.now].tolist() == [0, 0, 0] and int(d.books.state[d.books.now][1]) == d.books.ring.numel()
     more = torch.arange(3).mul(11)
     assert torch.equal(d.generate([more] * 3, 4), _decoder().generate([more] * 3, 4))
+
+
+def test_generate_raises_where_blocks_run_out():
+    for blocks, new in ((4, 2), (5, 10), (5, 14)):                 # the prompts take 1 + 3 + 1 blocks of 16; the second needs one more for its 49th token
+        d = _fewer_blocks(_decoder(), blocks)
+        with pytest.raises(RuntimeError):
+            d.generate(PROMPTS, new)
+    assert torch.equal(_fewer_blocks(_decoder(), 5).generate(PROMPTS, 9), _decoder().generate(PROMPTS, 9))
+
+
+def test_generate_raises_where_the_context_is_full():
+    d = _decoder(context=48)
+    assert d.generate(PROMPTS, 9).shape == (3, 9)                  # 40 tokens and eight behind them
+    with pytest.raises(ValueError):
+        d.generate(PROMPTS, 10)
+    d.step(torch.arange(4, device="cuda"), torch.tensor([0, 4, 0], dtype=torch.int32, device="cuda"), 4)
+    with pytest.raises(RuntimeError):                              # (with what the request held before)
+        d.generate(PROMPTS, 9)
