@@ -79,10 +79,12 @@ class Decoder:
         return B.linear_w4a16(x, self.head)[:, :len(self.tokens)]
 
     def generate(self, prompts, new: int) -> torch.Tensor:
-        """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids).  Requests
+        """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids, one or more each).  Requests
         go on from what they hold, and end with the call: their blocks are free again.  Raises where a request found no blocks, or
         no room in its context."""
         dev, n = self.tokens.device, [len(p) for p in prompts]
+        if len(n) != self.books.lens[0].numel() or not all(n) or new < 1:
+            raise ValueError(f"prompts of {n} tokens, {new} new ones: one prompt for each of {self.books.lens[0].numel()} requests, at least a token each")
         if max(n) + new - 1 > self.books.context:
             raise ValueError(f"{max(n)} tokens and {new - 1} behind them do not fit a context of {self.books.context}")
         ids, new_tokens = torch.cat([p.to(dev) for p in prompts]).long(), torch.tensor(n, dtype=torch.int32, device=dev)

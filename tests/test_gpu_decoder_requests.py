@@ -1,4 +1,4 @@
-"""Decoder.generate: requests that are not served, one call after the other."""
+"""Decoder.generate: requests that are not served, empty prompts, one call after the other."""
 import pytest
 import torch
 
@@ -45,3 +45,11 @@ def test_generate_raises_where_the_context_is_full():
     d.step(torch.arange(4, device="cuda"), torch.tensor([0, 4, 0], dtype=torch.int32, device="cuda"), 4)
     with pytest.raises(RuntimeError):                              # (with what the request held before)
         d.generate(PROMPTS, 9)
+
+
+def test_generate_refuses_prompts_that_are_none():
+    d = _decoder()
+    for prompts, new in (([PROMPTS[0], torch.arange(0), PROMPTS[2]], 3), ([torch.arange(0)] + PROMPTS[:2], 3), (PROMPTS[:2], 3), (PROMPTS, 0)):
+        with pytest.raises(ValueError):
+            d.generate(prompts, new)
+    assert d.books.lens[d.books.now].tolist() == [0, 0, 0]
