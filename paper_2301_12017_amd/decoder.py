@@ -14,12 +14,14 @@ from . import binding as B
 
 
 class Books:
-    """Which blocks the requests of a batch own: lengths, block table and the ring of free blocks, all on the device."""
+    """Which blocks the requests of a batch own: lengths, block table and the ring of free blocks, all on the device.  A request holds up to
+    `context` tokens, rounded up to whole blocks."""
 
     def __init__(self, requests: int, context: int, blocks: int, block=16, device="cuda"):
         z = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)
-        self.block, self.context = block, context
-        self.table, self.ring = z(requests, -(-context // block)), torch.arange(blocks, dtype=torch.int32, device=device)
+        width = -(-context // block)
+        self.block, self.context = block, width * block
+        self.table, self.ring = z(requests, width), torch.arange(blocks, dtype=torch.int32, device=device)
         self.lens, self.state = [z(requests), z(requests)], [torch.tensor([0, blocks], dtype=torch.int32, device=device), z(2)]
         self.now = 0                                       # which of the two holds the present
         self.workspace = B.KV8Workspace()                  # of the layers' attention, one after the other
@@ -62,6 +64,8 @@ class Decoder:
     """Token and position embeddings, layers, and the logits of the tokens' successors from the quantized token embeddings."""
 
     def __init__(self, layers, tokens: torch.Tensor, positions: torch.Tensor, books: Books, group=128):
+        if len(positions) < books.context:                 # (the plan hands out every position of a block, and they are looked up unseen)
+            raise ValueError(f"{len(positions)} position embeddings for requests of up to {books.context} tokens")
         self.layers, self.tokens, self.positions, self.books = layers, tokens, positions, books
         pad = -len(tokens) % 8                             # (the linear's channels come in eights)
         self.head = B.quantize_weight(torch.nn.functional.pad(tokens, (0, 0, 0, pad)).contiguous(), B.SYM, group)
@@ -108,11 +112,12 @@ def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabul
     g = torch.Generator(device="cuda").manual_seed(seed)
     normal = lambda *shape, std=0.02: (torch.randn(shape, generator=g, device="cuda") * std).half()
     D, blocks = hidden // heads, requests * -(-context // block)
+    books = Books(requests, context, blocks, block)
     one = lambda: (1 + normal(hidden, std=0.05).float()).half()
     made = [DecoderLayer(normal((heads + 2 * kv_heads) * D, hidden, std=0.05), normal((heads + 2 * kv_heads) * D), normal(hidden, heads * D), normal(hidden),
                          normal(ffn, hidden), normal(ffn), normal(hidden, ffn), normal(hidden), one(), normal(hidden), one(), normal(hidden),
                          heads, kv_heads, blocks, block, group, mode) for _ in range(layers)]
-    return Decoder(made, normal(vocabulary, hidden, std=1.0), normal(context, hidden, std=0.3), Books(requests, context, blocks, block), group)
+    return Decoder(made, normal(vocabulary, hidden, std=1.0), normal(books.context, hidden, std=0.3), books, group)
 
 
 if __name__ == "__main__":

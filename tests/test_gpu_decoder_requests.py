@@ -53,3 +53,9 @@ def test_generate_refuses_prompts_that_are_none():
         with pytest.raises(ValueError):
             d.generate(prompts, new)
     assert d.books.lens[d.books.now].tolist() == [0, 0, 0]
+
+
+def test_requests_fill_their_last_block_whatever_the_context():
+    d = _decoder(context=40)                                       # three blocks of 16: 48 tokens
+    found = d.generate(PROMPTS, 9)
+    assert torch.equal(found, _decoder(context=48).generate(PROMPTS, 9))
