@@ -546,6 +546,7 @@ typedef enum { W4A4_F16 = 0, W4A4_BF16 = 1 } w4a4_dtype;
  * X [M, ldx] (ldx elements, a multiple of 8), W canonical codes of either mode, one scale per channel or per group of a multiple
  * of 32 codes (rowsum_deq and esum are not read), bias may be NULL, out dense; pointers 16-byte aligned.  Meant for up to 64
  * tokens (W is read again for every 64, and for every 32 in groups that are no multiple of 128).  act: w4a4_act_fn, GELU on the fp32 value.
+ * The sums hold the codes with their offset (8 to 136), which leaves again: their roundings are those of sums up to 50 times the result.
  * Infinities and NaN in X come out as the sum of products has them (an infinity times a weight of 0 is NaN), in their rows alone. */
 int w4a4_linear_w4a16(const void *X, int dtype, int M, int K, int ldx, const w4a4_weight *W, const void *bias, int act,
                       void *out, void *stream);
@@ -612,7 +613,10 @@ typedef struct {
  * over its keys in the cache, and the logarithm of the sum of exp(score).  A query that sees nothing (a request of no
  * keys, a row that pads the batch) gets zeros and -infinity.  Rows of tokens that belong to no request are not written.
  * `queries` must hold (of a request that has more, nothing is promised but which rows are written: at most its own); keys past `context` only cost time.  A table entry that names no block
- * of the cache hides its keys.  A block whose scale is no finite number makes NaN of the rows that see one of its keys, output and
+ * of the cache hides its keys.  Scores, maxima and sums are fp32.  Weights, with the scale of their values in them, are rounded to fp16 (2^-11
+ * of each); products of weight and scale below 2^-27 of their row's largest (2^-20 for requests of many rows: more than 64 of a key head, in some
+ * batches more than 16) lose bits, 2^-11 of that bound each.  Where scales of a head's values are 2^80 apart, or below 2^-80, more is lost.
+ * bf16 queries lose what is 2^28 below the largest number of their head.  A block whose scale is no finite number makes NaN of the rows that see one of its keys, output and
  * logarithm, and of no others.  The workspace (16-byte aligned): its first 18432 bytes are zeros before its first use, and every call leaves
  * them so; it belongs to one call at a time, any that it is large enough for. */
 size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q);

@@ -9,9 +9,10 @@
 // two neighbouring features (one where D is 64) of sixteen tokens and writes each feature's codes as one sixteen-byte
 // piece of the block.  A run of at most sixteen tokens is read once, a longer one a second time out of L2.
 //
-// Memory bounds long runs: 12005 tokens of 8 heads of 128 features in blocks of 16, fp16, 28.6 us = 2.6 TB/s of 74 MB, since a run's range is known
-// only when its last token has come, and its codes follow in a second step; reading them back
-// 18.0 us = 4.1 TB/s.  Single tokens are latency, slots to scale to codes: 48 of 8 heads 4.5 us, and 4.6 to read 832.
+// Long runs: 12005 tokens of 8 heads of 128 features in blocks of 16, fp16, 28.6 us = 2.6 TB/s of 74 MB.  A wave takes its runs one after the
+// other, and in each the rows, their range, the scale and the codes are steps in series, of the keys with a load of the slot in front of
+// each store; other waves fill in.  Reading them back 18.0 us = 4.1 TB/s.  Single tokens are latency, slots to scale to codes: 48 of 8 heads 4.5 us where
+// most scales stay, 6.0 where all of them rise and their blocks are re-scaled (the long runs, of which few meet older codes: 2.1 more); 4.6 to read 832.
 #include "gen.hpp"
 
 namespace w4a4 {

@@ -26,8 +26,8 @@
 // which one is its own.  The pieces of a group leave sum, maximum and unfinished output in the workspace, and the one that
 // comes last joins them, in their order (a counter says who that is, not in which order sums are taken).
 //
-// Measured (kernel alone): one request of 150001 keys, 8 heads of 128, 62.5 us = 4.9 TB/s, the rate of a large copy; 32 requests of
-// 160 to 5000 keys (168 MB), 43.6 us = 3.9 TB/s, of which the lengths, the pieces and the join are 4; one request of 777 keys, 7.4 us, which is
+// Measured (kernel trace, median): one request of 150001 keys, 8 heads of 128, 62.4 us = 4.9 TB/s, the rate of a large copy; 32 requests of
+// 160 to 5000 keys (168 MB), 43.5 us = 3.9 TB/s, of which the lengths, the pieces and the join are 4; one request of 777 keys, 7.1 us, which is
 // launch, the table's words, two steps of a wave one after the other and the sum over its eight waves.
 #include "kv8_attention.hpp"
 
@@ -61,7 +61,9 @@ __device__ __forceinline__ Cut cut_of(const AttnArgs &a, int entries, int least,
     const int lane = threadIdx.x & 63, per = (entries + 63) / 64, e0 = min(lane * per, entries), e1 = min(e0 + per, entries);
     auto plus = [](int x, int y) { return x + y; };
     // equal shares of all steps, and larger pieces until there are no more of them than places for workgroups (where groups are
-    // more than the places, a piece more for each place)
+    // more than the places, a piece more for each place).  Up to as many groups as places, that leaves few pieces for what is long: of 512
+    // places, with 8 heads, 32 requests of up to 5000 keys are cut at 1.3 times the fair share, 64 at 2, and where one of them has 100000 keys and the others 300, at 2
+    // (32 requests), 3.5 (48) or not at all (52 to 64); 65 requests have pieces of the fair share again.
     int mine = 0, only = 0;
     for (int i = e0; i < e1; ++i) mine += only = entry(i).steps;
     const float fair = (float)lanes_reduce<64>(mine, plus) * (float)a.H / (float)a.slots;

@@ -12,7 +12,8 @@ constexpr int kCounters = kSlots + kMostGroups;                    // in the wor
 constexpr int kFewRows = 64;
 // Requests from which on a call whose bound allows more rows launches both kernels, each for its requests.  us both | only the one for many rows,
 // 8 key heads of 128, groups of 4: 4 requests of 4000 keys, 100 queries and three single ones 50 | 58, all of 300 queries 157 | 152; 64 of
-// 2000, 1500 queries and 63 single ones 160 | 220.
+// 2000, 1500 queries and 63 single ones 160 | 220.  (With fewer requests a single token beside a prompt is one useful wave of eight; that was not measured
+// over a long cache.)
 constexpr int kMixed = 4;
 
 // n / d for n * d < 2^32, one multiplication (a division by a number that the kernel gets costs some forty instructions).

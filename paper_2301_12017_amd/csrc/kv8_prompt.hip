@@ -17,9 +17,9 @@
 //
 // Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a sum, half a
 // maximum and half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
-// scores (128 features).  Measured: 1500 queries of a request of 4100 keys and 751 of one of 3726, 32 heads on 8 of 128 features (124 GFLOP), 158 us + 13.6 us for the join
-// = 720 TFLOP/s over both (the profiler's own time of the first is 178 to 190); matrix pipe 30 %, vector ALU 45 % of the cycles, hardly at
-// the same time with two waves in a SIMD, and more do not fit its registers.
+// scores (128 features).  Measured: 1500 queries of a request of 4100 keys and 751 of one of 3726, 32 heads on 8 of 128 features (124 GFLOP), 172 us
+// for the call among others = 720 TFLOP/s (kernel trace: 178 to 188, and 13.4 for the join); matrix pipe 29 %, vector ALU 46 % of the cycles (counters), hardly
+// at the same time with two waves in a SIMD, and more do not fit its registers.
 //
 // A group is 32 NW rows of a request and key head.  Groups beyond whole rounds of the device's workgroups are cut into pieces,
 // whose outputs a second kernel joins by their sums, each of its workgroups a slice of a group.

@@ -18,9 +18,9 @@
 // four lanes read 64 bytes apart, 32 cache lines a load instead of 16).  Inside eight codes the order is free as long as both
 // operands agree: (w >> 4j) & 0x000F000F gives codes j and j + 4 of a word, so the pairs of x are put in that order.
 //
-// Measured (kernel alone): 32 tokens of 4096 to 16384 channels, groups of 128 with zeros, 17.2 us, its 39 MB at 2.3 TB/s, where the
-// conversions, the products and the codes' way take turns in a SIMD's two waves (without the loads of x, which stay in L2, it would be a
-// fifth shorter); 5 tokens 4096 x 4096 5.2 us and one token 768 x 768 3.0 us, mostly launch, first loads and the sum over waves.
+// Measured (kernel trace, median): 32 tokens of 4096 to 16384 channels, groups of 128 with zeros, 18.4 us, its 39 MB at 2.1 TB/s: two waves
+// a SIMD, which wait half of their cycles (vector ALU 23 %, matrix pipe 9 %); without the loads of x, which come out of L2, it is 14.2 (64
+// tokens 4096 x 4096: 14.0 and 8.9).  5 tokens 4096 x 4096 5.7 us and one token 768 x 768 3.3 us, mostly launch, first loads and the sum over waves.
 #include "gen.hpp"
 
 namespace w4a4 {
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void linear_w4a16_kernel(W4A16Args
     bool on[MT];
     // Rows whose bytes at the same place lie in the same half of a cache line are read in turn, one its first 64 bytes of 128, the next its
     // second ones: 16 lanes at once would else ask for one half only.  (All rows of a lane are alike: sixteen rows are a multiple of 128 bytes.)
-    // us with | without, N x K: 64 tokens 4096 x 4096 14.9 | 19.2, 16000 x 4096 24.5 | 27.4, 32 tokens 4096 x 4096 8.6 | 11.7, 5 tokens 5.8 | 5.7; the
-    // tiles of 32 tokens and 64 channels have no registers for it (16384 x 4096 19.4 | 18.2).
+    // us with | without, N x K: 64 tokens 4096 x 4096 14.0 | 19.7, 16000 x 4096 25.5 | 29.2, 32 tokens 4096 x 4096 8.5 | 11.1, 5 tokens 5.7 | 5.7, 2048 tokens
+    // 373 | 550; the tiles of 32 tokens and 64 channels have no registers for it (16384 x 4096 19.4 | 18.2).
     constexpr bool TURNS = !(MT == 2 && NT == 4);
     const uint32_t half = TURNS && ((uint32_t)((reinterpret_cast<uintptr_t>(a.x) + (size_t)(m0 + col) * a.ldx * 2) >> 6) ^ (uint32_t)col) & 1 ? 32 : 0;
 #pragma unroll
