@@ -13,7 +13,7 @@
 // fp16 numbers.  m is let fall behind by up to 2^8 before what has been summed is re-scaled: weights stay below 2^15.  (To look for weights
 // that are too large among the packed ones, and for a maximum only then, took 207 us where this takes 190.)  Scales are taken relative to
 // z, a power of two near the wave's first one that is not 0 (it follows one that is 2^96 above); a block 2^80 below z, or of scale 0, counts as one
-// 2^80 below.
+// 2^80 below, and outputs that such blocks alone can make, less than 2^-73 of 2^z, are zeros.
 //
 // Bound by the vector ALU between the products: per score an FMA, an exponential at a quarter of the rate, a sum, half a
 // maximum and half a conversion, and 1.25 instructions per code and workgroup, beside 16 matrix instructions of 32 cycles for 32 x 32
@@ -424,7 +424,14 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
 
         l = both_halves(l, add2);
         const AttnArgs b = again();
-        const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(z) / l : 0.0f;
+        const float inv = l != 0.0f ? __builtin_amdgcn_exp2f(z) / l : 0.0f, least = __builtin_amdgcn_exp2f(z + (kBelow + 7.0f));
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                o[f][i] *= inv;
+                o[f][i] = fabsf(o[f][i]) < least ? 0.0f : o[f][i];
+            }
         const bool mine = wrow + col < t.rows;
         const size_t at = ((size_t)(t.first + j) * b.H + h) * b.group.d + b.group.rest(row, j);
         if (it.pieces > 1) {                                       // [item][wave][four features][lane]: joined later
@@ -435,7 +442,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
                 for (int f = 0; f < FT; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        po[(4 * f + i) * 64] = float4_t{o[f][4 * i] * inv, o[f][4 * i + 1] * inv, o[f][4 * i + 2] * inv, o[f][4 * i + 3] * inv};
+                        po[(4 * f + i) * 64] = float4_t{o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]};
                 if (hl == 0) *reinterpret_cast<float2 *>(b.pml + (slot * ROWS + 32 * wave + col) * 2) = float2{m, l};
             }
             continue;
@@ -445,7 +452,7 @@ __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void kv8_prompt_kernel(A
         for (int f = 0; f < FT; ++f)
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-                auto two = [&](int k) { return (uint32_t)from_float<BF16>(o[f][k] * inv) | (uint32_t)from_float<BF16>(o[f][k + 1] * inv) << 16; };
+                auto two = [&](int k) { return (uint32_t)from_float<BF16>(o[f][k]) | (uint32_t)from_float<BF16>(o[f][k + 1]) << 16; };
                 const auto s0 = __builtin_amdgcn_permlane32_swap(two(4 * i), two(4 * i + 4), false, false);
                 const auto s1 = __builtin_amdgcn_permlane32_swap(two(4 * i + 2), two(4 * i + 6), false, false);
                 if (any && mine) *reinterpret_cast<u32x4_t *>(dst + 32 * f + 8 * (i + hl)) = u32x4_t{(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};

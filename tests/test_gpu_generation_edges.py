@@ -250,3 +250,36 @@ def test_a_workspace_is_not_filled_with_zeros(B, monkeypatch):
     call = B.PreparedKV8Attention(q, cache, table, *args, 300, 600, 0.09)
     call()
     assert call.workspace.numel() > 10 ** 8 and made and all(t.numel() * t.element_size() <= 18432 for t in made)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("n, keys, window, D", [(1, 100, 0, 64), (5, 99, 40, 128), (40, 100, 0, 64), (300, 900, 70, 128), (40, 200, 0, 256)])
+def test_blocks_of_scale_zero_add_nothing(B, n, keys, window, D, dtype):
+    """Codes under a scale of 0: rows that see no others get zeros, for the others the block's values are zeros; its keys count in the sums."""
+    g, t, block = _gen(n + keys), TYPES[dtype], 16
+    blocks = -(-keys // block)
+    cache = _random_cache(B, g, blocks, 2, block, D)
+    call = B.PreparedKV8Attention(torch.randn((n, 4, D), generator=g).to(t).cuda(), cache, torch.arange(blocks, dtype=torch.int32, device="cuda")[None],
+                                  torch.tensor([keys], dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, keys, D ** -0.5, window=window, want_lse=True)
+    call()
+    sums = call.lse.clone()
+    kept = cache.v_scale.clone()
+    for first in (0, blocks // 2, blocks):                         # blocks of scale 0: all, those before the middle and every other one behind it, every other one
+        cache.v_scale.copy_(kept)
+        cache.v_scale[:blocks - first] = 0
+        cache.v_scale[::2] = 0
+        call()
+        with_codes, lse = call.out.clone(), call.lse.clone()
+        held = cache.v.clone()
+        cache.v[cache.v_scale[:, 0] == 0] = 0
+        call()
+        cache.v.copy_(held)
+        # (the codes may decide a rounding of what lies in the middle between two numbers: a step)
+        assert torch.equal(lse, call.lse) and torch.all((with_codes - call.out).abs().float() <= torch.finfo(t).eps * call.out.abs().float() + torch.finfo(t).smallest_normal * torch.finfo(t).eps)
+        at = keys - n + torch.arange(n)
+        begin = (at - window + 1).clamp(min=0) if window else at * 0
+        live = [any(float(cache.v_scale[b, 0]) > 0 for b in range(int(b0) // block, int(e) // block + 1)) for b0, e in zip(begin, at)]
+        none = ~torch.tensor(live).cuda()
+        assert not with_codes[none].any() and (bool(none.all()) or bool(with_codes[~none].any()))
+        # the sums do not depend on the scales but for their roundings: in the log a few of numbers below 2^7 and 2^-22 of the exponential
+        assert torch.all((lse - sums).abs() <= 300 * U + 2.0 ** -21 + (keys / 16 + 40) * U)
