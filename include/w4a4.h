@@ -615,7 +615,7 @@ typedef struct {
  * `queries` must hold (of a request that has more, nothing is promised but which rows are written: at most its own); keys past `context` only cost time.  A table entry that names no block
  * of the cache hides its keys.  Scores, maxima and sums are fp32.  Weights, with the scale of their values in them, are rounded to fp16 (2^-11
  * of each); products of weight and scale below 2^-27 of their row's largest (2^-20 for requests of many rows: more than 64 of a key head, in some
- * batches more than 16) lose bits, 2^-11 of that bound each.  Where scales of a head's values are 2^80 apart, or below 2^-80, more is lost.
+ * batches more than 16) lose bits, 2^-11 of that bound each.  Where scales of a head's values are 2^60 apart, or below 2^-80, more is lost.
  * bf16 queries lose what is 2^28 below the largest number of their head.  A block whose scale is no finite number makes NaN of the rows that see one of its keys, output and
  * logarithm, and of no others.  The workspace (16-byte aligned): its first 18432 bytes are zeros before its first use, and every call leaves
  * them so; it belongs to one call at a time, any that it is large enough for. */
