@@ -12,8 +12,9 @@ embeddings ends.  Five kinds of work:
   append     keys turned by their positions and values into the 8-bit cache, the step's queries turned as well, and the touched blocks
              read back.
 
-An operand in 4 bits is codes [rows, K / 2] (element 2j in the low four bits of byte j; sign, two bits of exponent, one of mantissa) and
-scales [ceil(K / 128), rows] in words of four: byte j of word [c, r] is 127 + the exponent of row r's numbers 128 c + 32 j and the 31 after.
+An operand in 4 bits is codes [ceil(K / 128), rows, 64] (row r's numbers 128 c .. 128 c + 127 in q[c, r], number 2j in the low four bits of
+byte j; sign, two bits of exponent, one of mantissa; zeros behind K) and scales [ceil(K / 128), rows] in words of four: byte j of word
+[c, r] is 127 + the exponent of row r's numbers 128 c + 32 j and the 31 after.
 """
 import math
 import random
@@ -127,20 +128,21 @@ def _grid(x):
     return index.int(), exponent
 
 
-def _words(exponent):
-    """Scale words [ceil(K / 128), rows] of exponents [rows, K / 32, 1]."""
-    rows, n = exponent.shape[:2]
-    e = torch.zeros((rows, (n + 3) // 4 * 4), dtype=torch.uint8, device="cuda")
-    e[:, :n] = (exponent[..., 0] + 127).to(torch.uint8)
-    return e.view(rows, -1, 4).permute(1, 0, 2).contiguous().view(torch.int32)[..., 0].contiguous()
+def _planes(x):
+    """x [rows, n, ...] with rows and groups of four of the n in each other's place, zeros behind the last: [ceil(n / 4), rows, 4, ...]."""
+    rows, n = x.shape[:2]
+    full = torch.zeros((rows, (n + 3) // 4 * 4, *x.shape[2:]), dtype=x.dtype, device="cuda")
+    full[:, :n] = x
+    return full.view(rows, -1, 4, *x.shape[2:]).transpose(0, 1).contiguous()
 
 
 def _operand(x):
     """Codes and scale words of x [rows, K]: a layer's weights, or activations that an earlier call has quantized."""
     x = x.float()
     index, exponent = _grid(x)
-    codes = (index + 8 * torch.signbit(x).view(index.shape)).view(x.shape[0], -1, 2).to(torch.uint8)
-    return {"q": (codes[..., 0] | codes[..., 1] << 4).contiguous(), "scale": _words(exponent)}
+    codes = (index + 8 * torch.signbit(x).view(index.shape)).to(torch.uint8)
+    return {"q": _planes(codes[..., 0::2] | codes[..., 1::2] << 4).flatten(2), "K": x.shape[1],
+            "scale": _planes((exponent[..., 0] + 127).to(torch.uint8)).view(torch.int32)[..., 0].contiguous()}
 
 
 def _prepare_quantize(case, r):
@@ -165,8 +167,8 @@ def _prepare_linear(case, r):
         from paper_2301_12017_amd import binding as B
         act = B.ACT_GELU if case["gelu"] else B.ACT_NONE
         first = [B.PreparedMX4Quantize(X)] if case["from_x"] else []
-        A = first[0].out if first else B.MX4(s["A"]["q"], s["A"]["scale"])
-        s["calls"] = first + [B.PreparedMX4Linear(A, B.MX4(s["W"]["q"], s["W"]["scale"]), s["bias"], act, dtype)]
+        A = first[0].out if first else B.MX4(s["A"]["q"], s["A"]["scale"], case["K"])
+        s["calls"] = first + [B.PreparedMX4Linear(A, B.MX4(s["W"]["q"], s["W"]["scale"], case["K"]), s["bias"], act, dtype)]
     return s
 
 
@@ -176,7 +178,7 @@ def _prepare_a16(case, r):
          "gelu": case["gelu"], "dtype": dtype}
     if own:
         from paper_2301_12017_amd import binding as B
-        s["calls"] = [B.PreparedMX4LinearA16(s["X"], B.MX4(s["W"]["q"], s["W"]["scale"]), s["bias"], B.ACT_GELU if case["gelu"] else B.ACT_NONE)]
+        s["calls"] = [B.PreparedMX4LinearA16(s["X"], B.MX4(s["W"]["q"], s["W"]["scale"], case["K"]), s["bias"], B.ACT_GELU if case["gelu"] else B.ACT_NONE)]
     return s
 
 
@@ -255,11 +257,11 @@ def prepare(case, seed):
 # ---- the plain forms ---------------------------------------------------------------------------------------------------
 def _values(Q):
     """The numbers [rows, K] that codes and scales stand for, in fp32."""
-    q, rows = Q["q"].to(torch.int32), Q["q"].shape[0]
-    codes = torch.stack([q & 15, q >> 4], -1).view(rows, -1, 32)
-    exponent = Q["scale"][..., None].contiguous().view(torch.uint8).permute(1, 0, 2).reshape(rows, -1)[:, :codes.shape[1]].int() - 127
+    q, rows = Q["q"].to(torch.int32), Q["q"].shape[1]
+    codes = torch.stack([q & 15, q >> 4], -1).view(-1, rows, 4, 32)
+    exponent = Q["scale"][..., None].contiguous().view(torch.uint8).int() - 127
     v = torch.tensor([*E2M1, *(-x for x in E2M1)], device="cuda")[codes]
-    return torch.ldexp(v, exponent[..., None]).view(rows, -1)
+    return torch.ldexp(v, exponent[..., None]).transpose(0, 1).reshape(rows, -1)[:, :Q["K"]]
 
 
 def _plain_quantize(x):
@@ -388,15 +390,16 @@ def _exact_rounded(x):
 
 
 def _exact_operand(Q):
-    q, rows = Q["q"], Q["q"].shape[0]
-    out = torch.empty((rows, 2 * q.shape[1]), dtype=torch.float64, device="cuda")
-    for parity in (0, 1):
-        c = q // 16 if parity else q % 16
-        e, m = (c // 2 % 4).double(), (c % 2).double()
-        out[:, parity::2] = torch.where(c >= 8, -1.0, 1.0) * torch.where(e == 0, m / 2, (1 + m / 2) * torch.exp2(e - 1))
-    for j in range(out.shape[1] // 32):
+    q, rows = Q["q"], Q["q"].shape[1]
+    out = torch.empty((rows, Q["K"]), dtype=torch.float64, device="cuda")
+    for j in range(Q["K"] // 32):
         byte = torch.bitwise_right_shift(Q["scale"][j // 4], 8 * (j % 4)) & 255
-        out[:, 32 * j:32 * j + 32] *= torch.exp2(byte.double() - 127)[:, None]
+        for parity in (0, 1):
+            c = q[j // 4, :, 16 * (j % 4):16 * (j % 4) + 16]
+            c = c // 16 if parity else c % 16
+            e, m = (c // 2 % 4).double(), (c % 2).double()
+            v = torch.where(c >= 8, -1.0, 1.0) * torch.where(e == 0, m / 2, (1 + m / 2) * torch.exp2(e - 1))
+            out[:, 32 * j + parity:32 * j + 32:2] = v * torch.exp2(byte.double() - 127)[:, None]
     return out
 
 
