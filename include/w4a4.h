@@ -594,6 +594,37 @@ int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const void *V, int d
 /* Keys and values of `tokens` slots, K and V [tokens, heads, features] in `dtype`; zeros for what is no slot. */
 int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream);
 
+/* Rotary positions: pairs of features turn by position * frequency,  a' = m (a cos - b sin),  b' = m (b cos + a sin).  Only the fraction of a
+ * turn counts: frequencies are in units of 2^-64 of a turn (angle a position / 2 pi * 2^64, rounded, modulo 2^64), so that a position, however far, loses nothing.
+ * Any scaling for long contexts is a matter of the frequencies and of the magnitude m. */
+typedef struct {
+    const uint64_t *turns;  /* [pairs] turn of each pair at position 1 (device)                */
+    int pairs;              /* of a head; 2 * pairs <= features: the features behind stay      */
+    int interleaved;        /* 1: pair i is features 2i and 2i + 1; 0: features i and i + pairs */
+    float magnitude;        /* m > 0                                                           */
+    int inverse;            /* 1: by the opposite angles, which takes gradients back (and, m being 1, turned rows) */
+} w4a4_rotary_angles;
+
+/* out[t, h, :] = X[t, h, :] turned by positions[t]; X and out in `dtype`, rows of heads * features numbers ldx and ldo elements apart (multiples of 8);
+ * out may be X (ldo == ldx), else the two do not overlap.  Rows of a negative position are copied.  Angles and products are fp32 (2^-22 of a pair's
+ * length in all), the result is rounded once.  features: a multiple of 8, 256 at most.  Fastest where pairs is a multiple of 8 or pairs are neighbours. */
+int w4a4_rotary(const void *X, int dtype, int tokens, int heads, int features, int ldx, const int32_t *positions,
+                const w4a4_rotary_angles *R, void *out, int ldo, void *stream);
+
+/* The rows of a step's new tokens. */
+typedef struct {
+    const void *k, *v;          /* [tokens, heads of the cache * features], rows ldk and ldv elements apart   */
+    const void *q;              /* [tokens, heads * features], rows ldq elements apart; NULL: no queries      */
+    void       *q_out;          /* [tokens, heads * features]: the queries turned, dense; overlaps nothing else; NULL without q */
+    const int32_t *slots;       /* [tokens] as for w4a4_kv8_append                                           */
+    const int32_t *positions;   /* [tokens] as for w4a4_rotary                                               */
+    int dtype, tokens, ldk, ldv, heads, ldq;    /* heads and ldq: of the queries                              */
+} w4a4_kv8_rows;
+
+/* w4a4_kv8_append with the keys turned by their positions on the way (in fp32: they are rounded once, to their codes; turned numbers that are not
+ * finite are stored as w4a4_kv8_append stores such), and w4a4_rotary of the step's queries. */
+int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_rows *T, const w4a4_rotary_angles *R, void *stream);
+
 /* The queries of an attention call. */
 typedef struct {
     const void    *q;       /* [tokens, ldq]: the first heads * features elements of a row     */
@@ -623,6 +654,33 @@ size_t w4a4_kv8_attention_workspace_bytes(const w4a4_kv8_cache *C, const w4a4_kv
 int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void *out, float *lse, void *workspace,
                        size_t workspace_bytes, void *stream);
 
+/* ---- microscaled 4-bit floating point ---------------------------------------------------------
+ * The 4-bit format that gfx950's matrix instruction takes as it is: E2M1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) of which 32
+ * neighbours of a row share a power of two.  Both operands in it: products at four times the rate of 16-bit ones; activations as they
+ * are: 17/32 byte of a weight to read.  One layout serves activations and weights, few tokens and many. */
+typedef struct {
+    uint8_t  *q;        /* [ceil(K/128), rows, 64]: q[c][r] holds numbers 128c .. 128c+127 of row r, number 2j in bits 0..3 of byte j
+                           and 2j+1 in bits 4..7 (sign, two bits of exponent, one of mantissa); zeros behind K      */
+    uint32_t *scale;    /* [ceil(K/128), rows]: byte j of scale[c][r] is 127 + the exponent of row r's block 4c + j; 255: the block is NaN; 0 behind K */
+    int rows, K;        /* K: a multiple of 32                                                                   */
+} w4a4_mx4;
+
+/* Rows X [out->rows, ldx] (first out->K columns) in `dtype` to out.  A block's exponent is floor(log2(its largest magnitude)) - 2, -127 at least; its numbers
+ * are rounded to the nearest, ties to the even mantissa, 6 at most in magnitude; the sign of what becomes zero stays.  A block with an infinity or a
+ * NaN is NaN.  Activations at run time, weights offline.  ldx a multiple of 8, pointers 16-byte aligned. */
+int w4a4_mx4_quantize(const void *X, int dtype, int ldx, const w4a4_mx4 *out, void *stream);
+
+/* The numbers that Q stands for, X [rows, K] in `dtype` (bf16 holds them exactly from 2^-126 on; fp16 rounds, and what passes it is an infinity). */
+int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *stream);
+
+/* out[M,N] = act(A * W^T + bias[N]), A [M, K] and W [N, K], bias (may be NULL) and out in `dtype`, fp32 sums, GELU on the fp32 value.
+ * N a multiple of 8; out dense, 16-byte aligned as the operands' codes and the bias are. */
+int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream);
+
+/* The same with activations X [M, ldx] (first W->K columns) in `dtype`, not quantized: for up to 64 tokens, where the bytes of W are the cost (W is read again for
+ * every 64).  A block's 32 products are summed before its power of two comes to them: an |x| past 2^120 may pass fp32 there.  ldx a multiple of 8. */
+int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, const w4a4_mx4 *W, const void *bias, int act, void *out, void *stream);
+
 /* A call of one of the entry points with its arguments laid out once, for callers to whom passing a dozen of them costs as
  * much as the launch (through Python's ctypes 1.5 us and more, of this 0.3).  p, i, f and n hold the entry point's pointers,
  * ints, float and size in the order of its parameters, the stream excepted; structs that a pointer names must still be there when
@@ -630,7 +688,9 @@ int w4a4_kv8_attention(const w4a4_kv8_cache *C, const w4a4_kv8_queries *Q, void 
 typedef enum {
     W4A4_CALL_QUANTIZE_ACT = 0, W4A4_CALL_LINEAR = 1, W4A4_CALL_LINEAR_F16ACT = 2, W4A4_CALL_LAYERNORM_QUANTIZE = 3,
     W4A4_CALL_QUANTIZE_ROWS8 = 4, W4A4_CALL_LINEAR8 = 5,       /* w8a8_quantize_rows, w8a8_linear */
-    W4A4_CALL_LINEAR_W4A16 = 6, W4A4_CALL_KV8_PLAN = 7, W4A4_CALL_KV8_APPEND = 8, W4A4_CALL_KV8_READ = 9, W4A4_CALL_KV8_ATTENTION = 10
+    W4A4_CALL_LINEAR_W4A16 = 6, W4A4_CALL_KV8_PLAN = 7, W4A4_CALL_KV8_APPEND = 8, W4A4_CALL_KV8_READ = 9, W4A4_CALL_KV8_ATTENTION = 10,
+    W4A4_CALL_ROTARY = 11, W4A4_CALL_KV8_APPEND_ROTARY = 12, W4A4_CALL_MX4_QUANTIZE = 13, W4A4_CALL_MX4_DEQUANTIZE = 14, W4A4_CALL_MX4_LINEAR = 15,
+    W4A4_CALL_MX4_LINEAR_A16 = 16
 } w4a4_call_entry;
 typedef struct {
     void *p[10];

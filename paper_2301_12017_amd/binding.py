@@ -6,8 +6,10 @@ memory and of the stream the kernels are enqueued on.  There is no CPU or
 PyTorch fallback: if the shared object is missing, loading fails.
 """
 import ctypes
+import math
 import os
 from dataclasses import dataclass
+from fractions import Fraction
 from typing import Optional
 
 import torch
@@ -87,6 +89,20 @@ class _KV8Queries(ctypes.Structure):
                 ("context", ctypes.c_int), ("window", ctypes.c_int)]
 
 
+class _RotaryAngles(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("pairs", ctypes.c_int), ("interleaved", ctypes.c_int), ("magnitude", ctypes.c_float), ("inverse", ctypes.c_int)]
+
+
+class _KV8Rows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("dtype", ctypes.c_int), ("tokens", ctypes.c_int), ("ldk", ctypes.c_int), ("ldv", ctypes.c_int),
+                ("heads", ctypes.c_int), ("ldq", ctypes.c_int)]
+
+
+class _MX4(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int), ("K", ctypes.c_int)]
+
+
 class _LayerWeights(ctypes.Structure):
     _fields_ = [("hidden", ctypes.c_int), ("heads", ctypes.c_int), ("ffn", ctypes.c_int),
                 ("qkv", _Part), ("attn_out", _Part), ("ffn1", _Part), ("ffn2", _Part),
@@ -146,6 +162,12 @@ _SIGNATURES = {
     "w4a4_kv8_read": (_i, [ctypes.POINTER(_KV8Cache), _vp, _i, _i, _vp, _vp, _vp]),
     "w4a4_kv8_attention_workspace_bytes": (_sz, [ctypes.POINTER(_KV8Cache), ctypes.POINTER(_KV8Queries)]),
     "w4a4_kv8_attention": (_i, [ctypes.POINTER(_KV8Cache), ctypes.POINTER(_KV8Queries), _vp, _vp, _vp, _sz, _vp]),
+    "w4a4_rotary": (_i, [_vp, _i, _i, _i, _i, _i, _vp, ctypes.POINTER(_RotaryAngles), _vp, _i, _vp]),
+    "w4a4_kv8_append_rotary": (_i, [ctypes.POINTER(_KV8Cache), ctypes.POINTER(_KV8Rows), ctypes.POINTER(_RotaryAngles), _vp]),
+    "w4a4_mx4_quantize": (_i, [_vp, _i, _i, ctypes.POINTER(_MX4), _vp]),
+    "w4a4_mx4_dequantize": (_i, [ctypes.POINTER(_MX4), _i, _vp, _vp]),
+    "w4a4_mx4_linear": (_i, [ctypes.POINTER(_MX4), ctypes.POINTER(_MX4), _vp, _i, _i, _vp, _vp]),
+    "w4a4_mx4_linear_a16": (_i, [_vp, _i, _i, _i, ctypes.POINTER(_MX4), _vp, _i, _vp, _vp]),
     "w4a4_run_call": (_i, [ctypes.POINTER(_Call), _vp]),
     "w4a4_dequant_epilogue": (_i, [_vp, ctypes.POINTER(_Act), ctypes.POINTER(_Weight),
                                    ctypes.POINTER(_Epilogue), _vp, _vp, _vp, _vp, _vp]),
@@ -444,7 +466,8 @@ class _Prepared:
     call on the current stream.  Handing the dozen arguments to the entry point itself took 1.5 us of the 3.8 that such a call
     cost on the host, more than the kernels of few tokens leave to hide it behind."""
     ENTRIES = ("w4a4_quantize_act", "w4a4_linear", "w4a4_linear_f16act", "w4a4_layernorm_quantize", "w8a8_quantize_rows", "w8a8_linear",
-               "w4a4_linear_w4a16", "w4a4_kv8_plan", "w4a4_kv8_append", "w4a4_kv8_read", "w4a4_kv8_attention")
+               "w4a4_linear_w4a16", "w4a4_kv8_plan", "w4a4_kv8_append", "w4a4_kv8_read", "w4a4_kv8_attention",
+               "w4a4_rotary", "w4a4_kv8_append_rotary", "w4a4_mx4_quantize", "w4a4_mx4_dequantize", "w4a4_mx4_linear", "w4a4_mx4_linear_a16")
 
     def _lay_out(self, name, pointers, ints=(), f=0.0, n=0):
         self.name = name
@@ -985,6 +1008,227 @@ def kv8_attention(q, cache, table, lens, start, queries: int, context: int, scal
     call = PreparedKV8Attention(q, cache, table, lens, start, queries, context, scale, window, want_lse, workspace=workspace)
     call()
     return (call.out, call.lse) if want_lse else call.out
+
+
+# ---- rotary positions --------------------------------------------------------------------------------
+class _PreparedOn(_Prepared):
+    """A prepared call that runs on its tensors' device, whatever the current one is: on that device's current stream."""
+
+    def _on(self, *tensors):
+        devices = {t.device for t in tensors if t is not None}
+        assert len(devices) == 1 and next(iter(devices)).type == "cuda", f"tensors on {devices}: one GPU"
+        self.device = next(iter(devices))
+
+    def __call__(self, stream=None):
+        if torch.cuda.current_device() == self.device.index:
+            return super().__call__(stream)
+        with torch.cuda.device(self.device):
+            return super().__call__(stream)
+
+
+def rotary_frequencies(pairs: int, base=10000.0, factor=1.0, trained=0, slow=1.0, fast=32.0):
+    """(radians a position of each pair [pairs], in 64 bits on the CPU, magnitude): base^(-i / pairs), for contexts `factor` times as long as a model was
+    trained on.  With `trained`, that length, each pair is scaled by how often it turns in it: more than `fast` times not at all, fewer than `slow` times
+    by the whole factor, between in proportion, and scores grow with the logarithm of the factor; without, positions are divided by the factor."""
+    if pairs <= 0 or not base > 0 or not factor >= 1 or trained < 0 or not fast > slow:
+        raise ValueError(f"{pairs} pairs, base {base}, factor {factor}, trained {trained}, slow {slow}, fast {fast}")
+    f = base ** (-torch.arange(pairs, dtype=torch.float64) / pairs)
+    if not trained:
+        return f / factor, 1.0
+    keep = ((trained * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+    return f * keep + f / factor * (1 - keep), 0.1 * math.log(factor) + 1.0
+
+
+class RotaryAngles:
+    """What w4a4_rotary turns by (w4a4_rotary_angles in include/w4a4.h): frequencies in radians a position, one for each pair (64 bits keep far positions
+    exact), pairs of neighbours or of halves, and what cosines and sines are multiplied by."""
+
+    def __init__(self, frequencies, interleaved=False, magnitude=1.0, device="cuda"):
+        f = torch.as_tensor(frequencies, dtype=torch.float64).cpu()
+        if f.dim() != 1 or not f.numel() or not torch.isfinite(f).all() or not 0 < magnitude < math.inf:
+            raise ValueError(f"frequencies {tuple(f.shape)}, finite ones in one dimension, and a magnitude above 0 ({magnitude})")
+        # of a turn, in 2^-64: whole turns do not count, and a negative fraction is the rest of a turn
+        turns = [round(Fraction(x) / _TWO_PI * 2 ** 64) % 2 ** 64 for x in f.tolist()]
+        self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64).to(device)
+        self.pairs, self.interleaved, self.magnitude = f.numel(), bool(interleaved), float(magnitude)
+
+    def c(self, inverse=False) -> _RotaryAngles:
+        return _RotaryAngles(_address(self.turns), self.pairs, int(self.interleaved), self.magnitude, int(bool(inverse)))
+
+
+_TWO_PI = 2 * Fraction("3.14159265358979323846264338327950288419716939937510")
+
+
+def _head_rows(x: torch.Tensor) -> int:
+    """Elements between the rows of x [tokens, heads, features]; the heads of a token lie together."""
+    T, H, D = x.shape
+    assert x.is_cuda and (D == 1 or x.stride(2) == 1) and (H == 1 or x.stride(1) == D)
+    return H * D if T <= 1 else x.stride(0)                                   # (of a single row the stride says nothing)
+
+
+class PreparedRotary(_PreparedOn):
+    """A w4a4_rotary call: X [tokens, heads, features] (a slice of a fused projection as it is) turned by its tokens' positions, in `out`, which may be X
+    itself.  inverse: by the opposite angles, which takes the gradient of the result to X's."""
+
+    def __init__(self, X: torch.Tensor, positions: torch.Tensor, angles: RotaryAngles, inverse=False, out: Optional[torch.Tensor] = None):
+        _i32(positions)
+        T, H, D = X.shape
+        assert positions.numel() >= T and 2 * angles.pairs <= D
+        if out is None:
+            out = torch.empty((T, H, D), dtype=X.dtype, device=X.device)
+        assert out.dtype == X.dtype and out.shape == X.shape
+        self._on(X, positions, angles.turns, out)
+        self.out, self.keep, self.c = out, (X, positions, angles), angles.c(inverse)
+        self._lay_out("w4a4_rotary", (X, positions, self.c, out), (_dtype(X.dtype), T, H, D, _head_rows(X), _head_rows(out)))
+
+
+def rotary(X: torch.Tensor, positions: torch.Tensor, angles: RotaryAngles, inverse=False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """w4a4_rotary: [tokens, heads, features] in the type of X."""
+    call = PreparedRotary(X, positions, angles, inverse, out)
+    call()
+    return call.out
+
+
+class PreparedKV8AppendRotary(_PreparedOn):
+    """A w4a4_kv8_append_rotary call: K, turned by the tokens' positions, and V [tokens, heads, features] into their slots, and queries
+    [tokens, heads, features] turned, in `q`.  Slices of a fused projection are taken as they are."""
+
+    def __init__(self, cache: KVCache8, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor, angles: RotaryAngles,
+                 q: Optional[torch.Tensor] = None):
+        _i32(slots, positions)
+        T = K.shape[0]
+        assert K.dtype == V.dtype and V.shape == K.shape and slots.numel() >= T and positions.numel() >= T and 2 * angles.pairs <= cache.features
+        assert q is None or (q.dtype == K.dtype and q.dim() == 3 and q.shape[0] == T and q.shape[2] == cache.features)
+        self._on(cache.k, cache.v, cache.k_scale, cache.v_scale, K, V, slots, positions, angles.turns, q)
+        self.q = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        self.keep, self.c, self.angles = (cache, K, V, slots, positions, angles, q), cache.c(), angles.c()
+        self.rows = _KV8Rows(_address(K), _address(V), _address(q), _address(self.q), _address(slots), _address(positions), _dtype(K.dtype), T,
+                             _kv_rows(cache, K), _kv_rows(cache, V), 0 if q is None else q.shape[1], 0 if q is None else _head_rows(q))
+        self._lay_out("w4a4_kv8_append_rotary", (self.c, self.rows, self.angles))
+
+
+def kv8_append_rotary(cache: KVCache8, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor, angles: RotaryAngles,
+                      q: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """w4a4_kv8_append_rotary; returns the queries turned, where there are any."""
+    call = PreparedKV8AppendRotary(cache, K, V, slots, positions, angles, q)
+    call()
+    return call.q
+
+
+# ---- microscaled 4-bit floating point ----------------------------------------------------------------
+class MX4:
+    """Rows of K numbers in microscaled 4-bit floating point (w4a4_mx4 in include/w4a4.h): codes q [ceil(K / 128), rows, 64] (uint8) and scale words
+    [ceil(K / 128), rows] (int32)."""
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, K: int):
+        planes, self.rows = scale.shape
+        self.K = K
+        assert K > 0 and K % 32 == 0 and planes == -(-K // 128) and q.shape == (planes, self.rows, 64), f"{tuple(q.shape)}, {tuple(scale.shape)}: planes of {K} numbers"
+        assert q.dtype == torch.uint8 and scale.dtype == torch.int32 and all(t.is_cuda and t.is_contiguous() for t in (q, scale))
+        self.q, self.scale = q, scale
+
+    @classmethod
+    def new(cls, rows: int, K: int, device="cuda"):
+        """Room for `rows` rows."""
+        planes = -(-K // 128)
+        return cls(torch.empty((planes, rows, 64), dtype=torch.uint8, device=device), torch.empty((planes, rows), dtype=torch.int32, device=device), K)
+
+    @classmethod
+    def from_rows(cls, codes: torch.Tensor, exponents: torch.Tensor):
+        """Of codes [rows, K / 2] (number 2j in the low four bits of byte j) and exponents [rows, K / 32] (plus 127, 255 for NaN), both uint8, as checkpoints
+        hold them."""
+        rows, half = codes.shape
+        assert codes.dtype == exponents.dtype == torch.uint8 and exponents.shape == (rows, half // 16) and half % 16 == 0
+        pad = -half % 64
+        q = torch.nn.functional.pad(codes, (0, pad)).view(rows, -1, 64).transpose(0, 1).contiguous()
+        e = torch.nn.functional.pad(exponents, (0, pad // 16)).view(rows, -1, 4).transpose(0, 1).contiguous()
+        return cls(q, e.view(torch.int32)[..., 0].contiguous(), 2 * half)
+
+    def c(self) -> _MX4:
+        return _MX4(_address(self.q), _address(self.scale), self.rows, self.K)
+
+
+def _rows16(X: torch.Tensor) -> int:
+    """Elements between the rows of X [rows, K]."""
+    assert X.is_cuda and X.dim() == 2 and (X.shape[1] == 1 or X.stride(1) == 1)
+    return X.shape[1] if X.shape[0] <= 1 else X.stride(0)
+
+
+class PreparedMX4Quantize(_PreparedOn):
+    """A w4a4_mx4_quantize call: rows X [rows, K] (fp16 or bf16, strided rows as they are); the result is in `out`."""
+
+    def __init__(self, X: torch.Tensor, out: Optional[MX4] = None):
+        rows, K = X.shape
+        self.out = MX4.new(rows, K, X.device) if out is None else out
+        assert (self.out.rows, self.out.K) == (rows, K)
+        self._on(X, self.out.q, self.out.scale)
+        self.keep, self.c = X, self.out.c()
+        self._lay_out("w4a4_mx4_quantize", (X, self.c), (_dtype(X.dtype), _rows16(X)))
+
+
+def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None) -> MX4:
+    call = PreparedMX4Quantize(X, out)
+    call()
+    return call.out
+
+
+class PreparedMX4Dequantize(_PreparedOn):
+    """A w4a4_mx4_dequantize call: the numbers [rows, K] that Q stands for, in `out`."""
+
+    def __init__(self, Q: MX4, dtype=torch.bfloat16):
+        self._on(Q.q, Q.scale)
+        self.out = torch.empty((Q.rows, Q.K), dtype=dtype, device=Q.q.device)
+        self.keep, self.c = Q, Q.c()
+        self._lay_out("w4a4_mx4_dequantize", (self.c, self.out), (_dtype(dtype),))
+
+
+def mx4_dequantize(Q: MX4, dtype=torch.bfloat16) -> torch.Tensor:
+    call = PreparedMX4Dequantize(Q, dtype)
+    call()
+    return call.out
+
+
+def _mx4_result(M: int, W: MX4, bias, dtype, out, device) -> torch.Tensor:
+    assert bias is None or (bias.dtype == dtype and bias.shape == (W.rows,) and bias.is_contiguous())
+    out = torch.empty((M, W.rows), dtype=dtype, device=device) if out is None else out
+    assert out.dtype == dtype and out.shape == (M, W.rows) and out.is_contiguous()
+    return out
+
+
+class PreparedMX4Linear(_PreparedOn):
+    """A w4a4_mx4_linear call: A [M, K] times W [N, K], both quantized; the result [M, N] is in `out`."""
+
+    def __init__(self, A: MX4, W: MX4, bias: Optional[torch.Tensor] = None, act=ACT_NONE, dtype=torch.float16, out: Optional[torch.Tensor] = None):
+        self.out = _mx4_result(A.rows, W, bias, dtype, out, A.q.device)
+        self._on(A.q, A.scale, W.q, W.scale, bias, self.out)
+        self.keep, self.a, self.w = (A, W, bias), A.c(), W.c()
+        self._lay_out("w4a4_mx4_linear", (self.a, self.w, bias, self.out), (act, _dtype(dtype)))
+
+
+def mx4_linear(A: MX4, W: MX4, bias: Optional[torch.Tensor] = None, act=ACT_NONE, dtype=torch.float16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """w4a4_mx4_linear: [M, N]."""
+    call = PreparedMX4Linear(A, W, bias, act, dtype, out)
+    call()
+    return call.out
+
+
+class PreparedMX4LinearA16(_PreparedOn):
+    """A w4a4_mx4_linear_a16 call: 16-bit activations X [M, K] of a few tokens times W [N, K]; the result, in the type of X, is in `out`."""
+
+    def __init__(self, X: torch.Tensor, W: MX4, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None):
+        M, K = X.shape
+        assert K == W.K
+        self.out = _mx4_result(M, W, bias, X.dtype, out, X.device)
+        self._on(X, W.q, W.scale, bias, self.out)
+        self.keep, self.w = (X, W, bias), W.c()
+        self._lay_out("w4a4_mx4_linear_a16", (X, self.w, bias, self.out), (_dtype(X.dtype), M, _rows16(X), act))
+
+
+def mx4_linear_a16(X: torch.Tensor, W: MX4, bias: Optional[torch.Tensor] = None, act=ACT_NONE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """w4a4_mx4_linear_a16: [M, N] in the type of X."""
+    call = PreparedMX4LinearA16(X, W, bias, act, out)
+    call()
+    return call.out
 
 
 def gemm_i32(A: QAct, W: QWeight, schedule=0) -> torch.Tensor:

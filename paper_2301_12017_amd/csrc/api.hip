@@ -38,6 +38,8 @@ extern "C" int w4a4_run_call(const w4a4_call *c, void *st) {
     auto f32 = [&](int k) { return static_cast<float *>(p[k]); };
     auto ep = [&](int k) { return static_cast<const w4a4_epilogue *>(p[k]); };
     auto cache = [&](int k) { return static_cast<const w4a4_kv8_cache *>(p[k]); };
+    auto angles = [&](int k) { return static_cast<const w4a4_rotary_angles *>(p[k]); };
+    auto mx4 = [&](int k) { return static_cast<const w4a4_mx4 *>(p[k]); };
     auto weight = [&](int k) { return static_cast<const w4a4_weight *>(p[k]); };
     switch (c->entry) {
         case W4A4_CALL_QUANTIZE_ACT:
@@ -62,6 +64,18 @@ extern "C" int w4a4_run_call(const w4a4_call *c, void *st) {
             return w4a4_kv8_read(cache(0), i32(1), i[0], i[1], p[2], p[3], st);
         case W4A4_CALL_KV8_ATTENTION:
             return w4a4_kv8_attention(cache(0), static_cast<const w4a4_kv8_queries *>(p[1]), p[2], f32(3), p[4], c->n, st);
+        case W4A4_CALL_ROTARY:
+            return w4a4_rotary(p[0], i[0], i[1], i[2], i[3], i[4], i32(1), angles(2), p[3], i[5], st);
+        case W4A4_CALL_KV8_APPEND_ROTARY:
+            return w4a4_kv8_append_rotary(cache(0), static_cast<const w4a4_kv8_rows *>(p[1]), angles(2), st);
+        case W4A4_CALL_MX4_QUANTIZE:
+            return w4a4_mx4_quantize(p[0], i[0], i[1], mx4(1), st);
+        case W4A4_CALL_MX4_DEQUANTIZE:
+            return w4a4_mx4_dequantize(mx4(0), i[0], p[1], st);
+        case W4A4_CALL_MX4_LINEAR:
+            return w4a4_mx4_linear(mx4(0), mx4(1), p[2], i[0], i[1], p[3], st);
+        case W4A4_CALL_MX4_LINEAR_A16:
+            return w4a4_mx4_linear_a16(p[0], i[0], i[1], i[2], mx4(1), p[2], i[3], p[3], st);
         default: return W4A4_ERR_INVALID_ARG;
     }
 }

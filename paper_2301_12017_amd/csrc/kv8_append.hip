@@ -13,7 +13,9 @@
 // other, and in each the rows, their range, the scale and the codes are steps in series, of the keys with a load of the slot in front of
 // each store; other waves fill in.  Reading them back 18.0 us = 4.1 TB/s.  Single tokens are latency, slots to scale to codes: 48 of 8 heads 4.5 us where
 // most scales stay, 6.0 where all of them rise and their blocks are re-scaled (the long runs, of which few meet older codes: 2.1 more); 4.6 to read 832.
-#include "gen.hpp"
+//
+// With positions, keys are turned (rotary.hpp) on their way in, in fp32: what is stored is the turned key rounded once, to its code.
+#include "rotary.hpp"
 
 namespace w4a4 {
 namespace {
@@ -27,6 +29,8 @@ struct AppendArgs {
     long ld[2];
     const int32_t *slots;
     int T, blocks, H, shift, tile;
+    const int32_t *positions;                                      // keys that turn
+    RotaryArgs r;
 };
 
 // Code of x.  CAREFUL, where infinities or NaN are among the tokens: NaN is stored as 0, an infinity as +-127.  Else |x| is at most
@@ -88,8 +92,54 @@ __device__ __forceinline__ float settle(float *scale, float had, int8_t *codes, 
     return now > 0.0f ? 1.0f / now : 0.0f;
 }
 
+// The features d .. d+7 of a key x (a lane's, in w) turned by its token's position.
+template <bool BF16>
+__device__ __forceinline__ void turn8(const RotaryArgs &r, const uint16_t *x, u32x4_t w, int d, int position, float (&to)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[j] = to_float<BF16>((uint16_t)(w[j / 2] >> (16 * (j % 2))));
+    if (position < 0) return;
+    if (r.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const int p = (d + j) / 2;
+            if (p >= r.pairs) break;
+            const Turn t = turn_of(r.turns[p], (uint32_t)position, r.magnitude, r.inverse);
+            const float u = to[j], v = to[j + 1];
+            to[j] = turned_a(t, u, v);
+            to[j + 1] = turned_b(t, u, v);
+        }
+        return;
+    }
+    if (d >= 2 * r.pairs) return;
+    uint32_t other[4];                                             // the partners: of halves that are whole pieces sixteen bytes
+    if (r.pairs % 8 == 0) {
+        const u32x4_t o = *reinterpret_cast<const u32x4_t *>(d < r.pairs ? x + r.pairs : x - r.pairs);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) other[j] = o[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            uint32_t o[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int f = d + j + e;
+                o[e] = x[f < r.pairs ? j + e + r.pairs : f < 2 * r.pairs ? j + e - r.pairs : j + e];
+            }
+            other[j / 2] = o[0] | o[1] << 16;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int f = d + j;
+        if (f >= 2 * r.pairs) break;
+        const Turn t = turn_of(r.turns[f < r.pairs ? f : f - r.pairs], (uint32_t)position, r.magnitude, r.inverse);
+        const float v = to_float<BF16>((uint16_t)(other[j / 2] >> (16 * (j % 2))));
+        to[j] = f < r.pairs ? turned_a(t, to[j], v) : turned_b(t, v, to[j]);
+    }
+}
+
 // Keys: tokens t0 .. t1-1 into the block's rows.
-template <bool BF16, int D>
+template <bool BF16, int D, bool ROTARY>
 __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane) {
     constexpr int LANES = D / 8, ROWS = 64 / LANES, N = (kPiece + ROWS - 1) / ROWS;   // lanes of a row, rows at once, loads of a chunk
     const int block = 1 << a.shift, row = lane / LANES;
@@ -99,6 +149,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
     int8_t *codes = a.k + unit * D * block;
     const float had = a.k_scale[unit];
     u32x4_t w[N];
+    float turned[ROTARY ? N : 1][8];
     auto load = [&](int c) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -106,22 +157,42 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
             w[i] = u32x4_t{0, 0, 0, 0};
             if (on && t < t1) w[i] = *reinterpret_cast<const u32x4_t *>(x + t * a.ld[0]);
         }
+        if constexpr (ROTARY)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int t = c + i * ROWS + row;
+                if (on && t < t1) turn8<BF16>(a.r, x + t * a.ld[0], w[i], lane % LANES * 8, a.positions[t], turned[i]);
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) turned[i][j] = 0.0f;
+            }
     };
-    auto range = [&](bool careful) {
+    auto range = [&](bool careful) {                               // (of turned keys the bits of an fp32 number)
         Range m;
+        uint32_t most = 0;
         for (int c = t0; c < t1; c += N * ROWS) {
             load(c);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int i = 0; i < N; ++i) {
+                if constexpr (ROTARY) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) m.take(careful ? finite2<BF16>(w[i][j]) : w[i][j]);
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t bits = __builtin_bit_cast(uint32_t, turned[i][j]) & 0x7FFFFFFFu;
+                        most = max(most, careful && bits >= 0x7F800000u ? 0u : bits);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) m.take(careful ? finite2<BF16>(w[i][j]) : w[i][j]);
+                }
+            }
         }
-        return m.over_wave();
+        if constexpr (ROTARY) return lanes_reduce<64>(most, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        else return m.over_wave();
     };
     uint32_t wide = range(false);
-    const bool careful = wide >= kInf<BF16>;
+    const bool careful = wide >= (ROTARY ? 0x7F800000u : kInf<BF16>);
     if (careful) wide = range(true);
-    const float inv = settle(a.k_scale + unit, had, codes, D * block, first, to_float<BF16>((uint16_t)wide), lane);
+    const float inv = settle(a.k_scale + unit, had, codes, D * block, first, ROTARY ? __builtin_bit_cast(float, wide) : to_float<BF16>((uint16_t)wide), lane);
     auto write = [&](auto careful) {
         constexpr bool C = decltype(careful)::value;
         for (int c = t0; c < t1; c += N * ROWS) {
@@ -132,7 +203,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
                 if (!on || t >= t1) continue;
                 uint32_t o[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = code8<C>(to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2)))), inv);
+                for (int j = 0; j < 8; ++j) o[j] = code8<C>(ROTARY ? turned[ROTARY ? i : 0][j] : to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2)))), inv);
                 *reinterpret_cast<u32x2_t *>(codes + (size_t)(a.slots[t] & (block - 1)) * D + lane % LANES * 8) =
                     u32x2_t{bytes4(o[0], o[1], o[2], o[3]), bytes4(o[4], o[5], o[6], o[7])};
             }
@@ -241,7 +312,7 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     else write(std::false_type{});
 }
 
-template <bool BF16, int D>
+template <bool BF16, int D, bool ROTARY>
 __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int which = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);   // 0 .. H-1: keys of a head, H .. 2H-1: values
@@ -279,7 +350,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
             }
         }
         const int off = __builtin_amdgcn_readlane(slot, i) & mask;
-        if (which < a.H) append_keys<BF16, D>(a, t0, t1, bi, which, first, lane);
+        if (which < a.H) append_keys<BF16, D, ROTARY>(a, t0, t1, bi, which, first, lane);
         else append_values<BF16, D>(a, t0, t1, bi, which - a.H, first, ordered, off, lane);
     }
 }
@@ -421,8 +492,10 @@ int kv8_cache_check(const w4a4_kv8_cache *C) {
 
 using namespace w4a4;
 
-extern "C" int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv,
-                               const int32_t *slots, void *stream) {
+namespace {
+
+// What both entry points ask of keys, values and slots.
+int rows_check(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv, const int32_t *slots) {
     if (const int rc = kv8_cache_check(C)) return rc;
     if (tokens < 0 || (dtype != W4A4_F16 && dtype != W4A4_BF16)) return W4A4_ERR_INVALID_ARG;
     const int row = C->heads * C->features;
@@ -430,15 +503,44 @@ extern "C" int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const voi
     if (tokens == 0) return W4A4_OK;
     if (!K || !V || !slots) return W4A4_ERR_INVALID_ARG;
     if (ldk % 8 || ldv % 8 || !aligned16(K) || !aligned16(V)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    return W4A4_OK;
+}
+
+template <bool ROTARY>
+int append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv, const int32_t *slots, const int32_t *positions,
+           const RotaryArgs &r, hipStream_t st) {
     AppendArgs a{C->k, C->v, C->k_scale, C->v_scale, {static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V)}, {ldk, ldv},
-                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece};
+                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece, positions, r};
     const dim3 grid((tokens + a.tile - 1) / a.tile, (2 * C->heads + 3) / 4);
     return by_features(C->features, [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (dtype == W4A4_BF16) hipLaunchKernelGGL((kv8_append_kernel<true, D>), grid, dim3(256), 0, as_stream(stream), a);
-        else hipLaunchKernelGGL((kv8_append_kernel<false, D>), grid, dim3(256), 0, as_stream(stream), a);
+        if (dtype == W4A4_BF16) hipLaunchKernelGGL((kv8_append_kernel<true, D, ROTARY>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((kv8_append_kernel<false, D, ROTARY>), grid, dim3(256), 0, st, a);
         return launch_status();
     });
+}
+
+}  // namespace
+
+extern "C" int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv,
+                               const int32_t *slots, void *stream) {
+    if (const int rc = rows_check(C, K, V, dtype, tokens, ldk, ldv, slots)) return rc;
+    if (tokens == 0) return W4A4_OK;
+    return append<false>(C, K, V, dtype, tokens, ldk, ldv, slots, nullptr, RotaryArgs{}, as_stream(stream));
+}
+
+extern "C" int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_rows *T, const w4a4_rotary_angles *R, void *stream) {
+    if (!T) return W4A4_ERR_INVALID_ARG;
+    if (const int rc = rows_check(C, T->k, T->v, T->dtype, T->tokens, T->ldk, T->ldv, T->slots)) return rc;
+    if (const int rc = rotary_check(R, C->features)) return rc;
+    if (T->q && (T->heads <= 0 || (long)T->heads * C->features > T->ldq)) return W4A4_ERR_INVALID_ARG;
+    if (T->tokens == 0) return W4A4_OK;
+    if (!T->positions || !T->q != !T->q_out || (T->q && T->q == T->q_out)) return W4A4_ERR_INVALID_ARG;
+    if (T->q && (T->ldq % 8 || !aligned16(T->q) || !aligned16(T->q_out))) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const RotaryArgs r = rotary_args(R);
+    if (const int rc = append<true>(C, T->k, T->v, T->dtype, T->tokens, T->ldk, T->ldv, T->slots, T->positions, r, as_stream(stream))) return rc;
+    if (!T->q) return W4A4_OK;
+    return rotary_launch(T->q, T->dtype, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, as_stream(stream));
 }
 
 extern "C" int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream) {

@@ -1,0 +1,41 @@
+// What the kernels of microscaled 4-bit floating point share (gfx950).
+//
+// A number is E2M1 (sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) times a power of two that it shares with 31
+// neighbours of its row.  Planes of 128 numbers: 64 bytes of codes and one word of four exponents (plus 127) for each row.
+#pragma once
+#include "gen.hpp"
+
+namespace w4a4 {
+
+typedef int v8i_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+
+constexpr int kPlane = 128;                                        // numbers of a row in a plane
+constexpr int kPlaneBytes = 64;
+
+inline int mx4_planes(int K) { return (K + kPlane - 1) / kPlane; }
+
+// 2^(e - 127) for the byte e; NaN for 255.
+__device__ __forceinline__ float mx4_scale(uint32_t e) {
+    const uint32_t bits = e ? e << 23 : 0x00400000u;
+    return __builtin_bit_cast(float, e == 255 ? 0x7FC00000u : bits);
+}
+
+// What both products do to a sum before it is rounded to the output's type.
+template <bool GELU>
+__device__ __forceinline__ float mx4_finish(float y, float bias) {
+    y += bias;
+    if (GELU && y == y) y = gelu_erf(y);                           // (which takes a NaN with its sign bit set for a negative number)
+    return y;
+}
+
+// W4A4_OK, or what is wrong with an operand.
+inline int mx4_check(const w4a4_mx4 *Q) {
+    if (!Q || Q->rows < 0 || Q->K <= 0) return W4A4_ERR_INVALID_ARG;
+    if (Q->rows && (!Q->q || !Q->scale)) return W4A4_ERR_INVALID_ARG;
+    if (Q->K % 32 || !aligned16(Q->q) || (reinterpret_cast<uintptr_t>(Q->scale) & 3)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    return W4A4_OK;
+}
+
+}  // namespace w4a4

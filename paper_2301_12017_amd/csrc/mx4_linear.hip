@@ -1,0 +1,124 @@
+// Linear layers whose operands are both microscaled 4-bit floating point.
+//
+//   y[m,n] = act( sum_blocks 2^(ea[m,b] + ew[n,b]) * sum_{k in b} a[m,k] w[n,k]  + bias[n] )
+//
+// The matrix instruction takes codes and exponents as they are: 128 numbers of 16 rows, a lane one block of one row, sixteen bytes of codes
+// and a byte of exponent.  A plane's rows follow each other, so such an operand is a kilobyte of consecutive memory.
+#include "mx4.hpp"
+
+namespace w4a4 {
+namespace {
+
+struct LinearArgs {
+    const uint8_t *a, *w;
+    const uint32_t *sa, *sw;
+    const uint16_t *bias;
+    uint16_t *out;
+    int M, N, planes, act, tiles_n;
+};
+
+__device__ __forceinline__ v8i_t operand(u32x4_t x) { return v8i_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
+
+// Few tokens: MT x NT tiles of 16 x 16, the waves of a workgroup have a part of K each and add up in LDS, in their order.
+template <bool BF16, int MT, int NT, int NW>
+__global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(LinearArgs a) {
+    extern __shared__ float red[];                                 // [NW][MT * NT * 4][64]
+    constexpr int AHEAD = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, kg = lane >> 4;
+    const int m0 = blockIdx.x / a.tiles_n * (16 * MT), n0 = blockIdx.x % a.tiles_n * (16 * NT);
+    const int each = (a.planes + NW - 1) / NW, c0 = wave * each, c1 = min(c0 + each, a.planes);
+    struct Stage {
+        u32x4_t x[MT], w[NT];
+        uint32_t sx[MT], sw[NT];
+    } st[AHEAD];
+    auto load = [&](Stage &s, int c) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const size_t at = (size_t)c * a.M + min(m0 + 16 * t + row, a.M - 1);
+            s.x[t] = *reinterpret_cast<const u32x4_t *>(a.a + at * kPlaneBytes + 16 * kg);
+            s.sx[t] = a.sa[at];
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const size_t at = (size_t)c * a.N + min(n0 + 16 * t + row, a.N - 1);
+            s.w[t] = *reinterpret_cast<const u32x4_t *>(a.w + at * kPlaneBytes + 16 * kg);
+            s.sw[t] = a.sw[at];
+        }
+    };
+    float4_t acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p)
+        if (c0 + p < c1) load(st[p], c0 + p);
+    for (int c = c0; c < c1; c += AHEAD) {
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p) {
+            if (c + p >= c1) break;
+            Stage &s = st[p];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(s.x[i]), operand(s.w[t]), acc[i][t], 4, 4, 0, (int)(s.sx[i] >> (8 * kg)), 0,
+                                                                                 (int)(s.sw[t] >> (8 * kg)));
+            if (c + p + AHEAD < c1) load(s, c + p + AHEAD);
+        }
+    }
+    constexpr int REGS = MT * NT * 4;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) red[(wave * REGS + (i * NT + t) * 4 + e) * 64 + lane] = acc[i][t][e];
+    __syncthreads();
+    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
+    for (int o = threadIdx.x; o < rows * 16 * NT; o += NW * 64) {
+        const int m = o / (16 * NT), n = o % (16 * NT);
+        if (n >= cols) continue;
+        const int reg = ((m >> 4) * NT + (n >> 4)) * 4 + (m & 3), from = ((m & 15) >> 2) * 16 + (n & 15);
+        float y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
+        const float bias = a.bias ? to_float<BF16>(a.bias[n0 + n]) : 0.0f;
+        a.out[(size_t)(m0 + m) * a.N + n0 + n] = from_float<BF16>(a.act == W4A4_ACT_GELU ? mx4_finish<true>(y, bias) : mx4_finish<false>(y, bias));
+    }
+}
+
+template <bool BF16, int MT, int NT, int NW>
+int launch_few(LinearArgs a, hipStream_t st) {
+    auto kern = mx4_linear_few_kernel<BF16, MT, NT, NW>;
+    constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
+    a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
+    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
+    if (tiles > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    static KernelState ks;
+    if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
+    return launch_status();
+}
+
+template <bool BF16>
+int pick(const LinearArgs &a, hipStream_t st) {
+    if (a.M <= 16) return launch_few<BF16, 1, 1, 8>(a, st);
+    return launch_few<BF16, 4, 2, 8>(a, st);
+}
+
+}  // namespace
+}  // namespace w4a4
+
+using namespace w4a4;
+
+extern "C" int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream) {
+    if (const int rc = mx4_check(A)) return rc;
+    if (const int rc = mx4_check(W)) return rc;
+    if (A->K != W->K || W->rows == 0 || (dtype != W4A4_F16 && dtype != W4A4_BF16) || (act != W4A4_ACT_NONE && act != W4A4_ACT_GELU)) return W4A4_ERR_INVALID_ARG;
+    if (A->rows == 0) return W4A4_OK;
+    if (!out) return W4A4_ERR_INVALID_ARG;
+    if (W->rows % 8 || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const LinearArgs a{A->q, W->q, A->scale, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), A->rows, W->rows, mx4_planes(A->K), act, 0};
+    return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
+}

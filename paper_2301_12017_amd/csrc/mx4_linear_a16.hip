@@ -1,0 +1,171 @@
+// Linear layers of few tokens: fp16 or bf16 activations as they are, weights in microscaled 4-bit floating point.
+//
+//   y[m,n] = act( sum_blocks 2^e[n,b] * sum_{k in b} w[n,k] x[m,k]  + bias[n] )
+//
+// A weight is read once, 17/32 byte of it, so the bytes of W bound the call.  Its codes become 16-bit numbers by a conversion instruction, two
+// at a time and exact (the exponents stay out: they pass what fp16 holds); 32 of them are one matrix instruction, whose sums in
+// fp32 go into the total with the block's power of two.
+//
+// A wave reads a plane of 16 channels as one kilobyte: a lane has a block, four words of eight codes.  The four lanes that share a channel
+// change words (two lane swaps a pair), so that each instruction has one block of all 16 channels and a row of x is read 64 bytes at a time.
+#include "mx4.hpp"
+
+namespace w4a4 {
+namespace {
+
+struct A16Args {
+    const uint16_t *x;
+    const uint8_t *w;
+    const uint32_t *sw;
+    const uint16_t *bias;
+    uint16_t *out;
+    int M, N, K, ldx, act, tiles_n;
+};
+
+// words (lane group g, j) -> (lane group j, word g) for the four groups of sixteen lanes
+__device__ __forceinline__ u32x4_t transpose_groups(u32x4_t w) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap((unsigned)a[0], (unsigned)b[0], false, false);
+    const auto d = __builtin_amdgcn_permlane16_swap((unsigned)a[1], (unsigned)b[1], false, false);
+    return u32x4_t{(unsigned)c[0], (unsigned)c[1], (unsigned)d[0], (unsigned)d[1]};
+}
+
+template <bool BF16>
+__device__ __forceinline__ u32x4_t numbers8(uint32_t w) {          // eight codes as 16-bit numbers
+    u32x4_t o;
+#define PAIR(J)                                                                                                                               \
+    if constexpr (BF16) o[J] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, J));                           \
+    else o[J] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, J));
+    PAIR(0) PAIR(1) PAIR(2) PAIR(3)
+#undef PAIR
+    return o;
+}
+
+template <bool BF16, int MT, int NT, int NW>
+__global__ __launch_bounds__(NW * 64) void mx4_linear_a16_kernel(A16Args a) {
+    extern __shared__ float red[];                                 // [NW][MT * NT * 4][64]
+    constexpr int AHEAD = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
+    const int m0 = blockIdx.x / a.tiles_n * (16 * MT), n0 = blockIdx.x % a.tiles_n * (16 * NT);
+    const int planes = (a.K + kPlane - 1) / kPlane, each = (planes + NW - 1) / NW, c0 = wave * each, c1 = min(c0 + each, planes);
+    struct Stage {
+        u32x4_t w[NT];
+        uint32_t s[NT];
+    } st[AHEAD];
+    auto load = [&](Stage &s, int c) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const size_t at = (size_t)c * a.N + min(n0 + 16 * t + col, a.N - 1);
+            s.w[t] = *reinterpret_cast<const u32x4_t *>(a.w + at * kPlaneBytes + 16 * kg);
+            s.s[t] = a.sw[at];
+        }
+    };
+    u32x4_t x[MT][4];
+    auto load_x = [&](int c) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const uint16_t *p = a.x + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.ldx + c * kPlane + 8 * kg;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[t][j] = u32x4_t{0, 0, 0, 0};
+                if (c * kPlane + 32 * j < a.K) x[t][j] = *reinterpret_cast<const u32x4_t *>(p + 32 * j);
+            }
+        }
+    };
+    float4_t tot[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) tot[i][t] = float4_t{0, 0, 0, 0};
+    auto compute = [&](Stage &s, int next) {
+        u32x4_t xr[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xr[i][j] = x[i][j];
+        if (next < c1) load_x(next);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const u32x4_t w4 = transpose_groups(s.w[t]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32x4_t w = numbers8<BF16>(w4[j]);
+                const float by = mx4_scale(s.s[t] >> (8 * j) & 255);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const float4_t sum = mfma16<BF16>(xr[i][j], w, float4_t{0, 0, 0, 0});
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) tot[i][t][e] = __fmaf_rn(sum[e], by, tot[i][t][e]);
+                }
+            }
+        }
+    };
+    if (c0 < c1) {
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p)
+            if (c0 + p < c1) load(st[p], c0 + p);
+        load_x(c0);
+        for (int c = c0; c < c1; c += AHEAD) {
+#pragma unroll
+            for (int p = 0; p < AHEAD; ++p) {
+                if (c + p >= c1) break;
+                compute(st[p], c + p + 1);
+                if (c + p + AHEAD < c1) load(st[p], c + p + AHEAD);
+            }
+        }
+    }
+    constexpr int REGS = MT * NT * 4;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) red[(wave * REGS + (i * NT + t) * 4 + e) * 64 + lane] = tot[i][t][e];
+    __syncthreads();
+    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
+    for (int o = threadIdx.x; o < rows * 16 * NT; o += NW * 64) {
+        const int m = o / (16 * NT), n = o % (16 * NT);
+        if (n >= cols) continue;
+        const int reg = ((m >> 4) * NT + (n >> 4)) * 4 + (m & 3), from = ((m & 15) >> 2) * 16 + (n & 15);
+        float y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
+        const float bias = a.bias ? to_float<BF16>(a.bias[n0 + n]) : 0.0f;
+        a.out[(size_t)(m0 + m) * a.N + n0 + n] = from_float<BF16>(a.act == W4A4_ACT_GELU ? mx4_finish<true>(y, bias) : mx4_finish<false>(y, bias));
+    }
+}
+
+template <bool BF16, int MT, int NT, int NW>
+int launch(A16Args a, hipStream_t st) {
+    auto kern = mx4_linear_a16_kernel<BF16, MT, NT, NW>;
+    constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
+    a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
+    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
+    if (tiles > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    static KernelState ks;
+    if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
+    return launch_status();
+}
+
+template <bool BF16>
+int pick(const A16Args &a, hipStream_t st) {
+    if (a.M <= 16) return launch<BF16, 1, 1, 8>(a, st);
+    return launch<BF16, 2, 1, 8>(a, st);
+}
+
+}  // namespace
+}  // namespace w4a4
+
+using namespace w4a4;
+
+extern "C" int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, const w4a4_mx4 *W, const void *bias, int act, void *out, void *stream) {
+    if (const int rc = mx4_check(W)) return rc;
+    if (M < 0 || ldx < W->K || W->rows == 0 || (dtype != W4A4_F16 && dtype != W4A4_BF16) || (act != W4A4_ACT_NONE && act != W4A4_ACT_GELU)) return W4A4_ERR_INVALID_ARG;
+    if (M == 0) return W4A4_OK;
+    if (!X || !out) return W4A4_ERR_INVALID_ARG;
+    if (W->rows % 8 || ldx % 8 || !aligned16(X) || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const A16Args a{static_cast<const uint16_t *>(X), W->q, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), M, W->rows, W->K, ldx, act, 0};
+    return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
+}
