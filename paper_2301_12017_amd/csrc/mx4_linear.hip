@@ -5,23 +5,16 @@
 // The matrix instruction takes codes and exponents as they are: 128 numbers of 16 rows, a lane one block of one row, sixteen bytes of codes
 // and a byte of exponent.  A plane's rows follow each other, so such an operand is a kilobyte of consecutive memory.
 #include "mx4.hpp"
+#include "mx4_linear.hpp"
 
 namespace w4a4 {
 namespace {
-
-struct LinearArgs {
-    const uint8_t *a, *w;
-    const uint32_t *sa, *sw;
-    const uint16_t *bias;
-    uint16_t *out;
-    int M, N, planes, act, tiles_n;
-};
 
 __device__ __forceinline__ v8i_t operand(u32x4_t x) { return v8i_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
 
 // Few tokens: MT x NT tiles of 16 x 16, the waves of a workgroup have a part of K each and add up in LDS, in their order.
 template <bool BF16, int MT, int NT, int NW>
-__global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(LinearArgs a) {
+__global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a) {
     extern __shared__ float red[];                                 // [NW][MT * NT * 4][64]
     constexpr int AHEAD = 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, kg = lane >> 4;
@@ -88,23 +81,53 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(LinearArgs a) {
     }
 }
 
+// A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us by tiles of one kind:
+// small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s of them, whatever is asked for at once), large ones bring less
+// in all.  The constants are fitted to 100 to 110 sizes of 1 to 16538 tokens; over 150 sizes the choice is 3 % above the best of fourteen kinds, 27 % at worst.
+struct Way {
+    int bm, bn;
+    float start, plane, more, tile;
+};
+constexpr int kFew = 3;                                            // the first of them are this file's, the others kMX4Tile..
+constexpr Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f},   {32, 32, 2.35f, 0.069f, 0.074f, 0.705f},
+                         {64, 64, 4.14f, 0.096f, 0.132f, 2.735f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f},
+                         {128, 256, 4.14f, 0.413f, 0.587f, 3.836f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f}};
+
+int way_of(const MX4LinearArgs &a, int cus) {
+    int best = 0;
+    float least = INFINITY;
+    const int ways = a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew;      // (the tiles in LDS have 32-bit offsets into the results)
+    for (int i = 0; i < ways; ++i) {
+        const Way &w = kWays[i];
+        const float tiles = (float)(((long)a.M + w.bm - 1) / w.bm) * (float)(((long)a.N + w.bn - 1) / w.bn), rest = tiles / (float)cus - 1.0f;
+        const float us = w.start + w.plane * (float)a.planes + (rest > 0.0f ? (w.more * (float)a.planes + w.tile) * rest : 0.0f);
+        if (us < least) least = us, best = i;
+    }
+    return best;
+}
+
 template <bool BF16, int MT, int NT, int NW>
-int launch_few(LinearArgs a, hipStream_t st) {
+int launch_few(MX4LinearArgs a, hipStream_t st) {
     auto kern = mx4_linear_few_kernel<BF16, MT, NT, NW>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
     const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
-    if (tiles > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    static KernelState ks;
-    if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
     return launch_status();
 }
 
 template <bool BF16>
-int pick(const LinearArgs &a, hipStream_t st) {
-    if (a.M <= 16) return launch_few<BF16, 1, 1, 8>(a, st);
-    return launch_few<BF16, 4, 2, 8>(a, st);
+int pick(const MX4LinearArgs &a, hipStream_t st) {
+    static KernelState ks;
+    const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_few_kernel<BF16, 1, 1, 8>), 0, ks);
+    if (cus < 0) return W4A4_ERR_HIP;
+    const int way = way_of(a, cus);
+    switch (way) {
+        case 0: return launch_few<BF16, 1, 1, 8>(a, st);
+        case 1: return launch_few<BF16, 1, 2, 8>(a, st);
+        case 2: return launch_few<BF16, 2, 2, 8>(a, st);
+        default: return mx4_tiles(a, BF16 ? W4A4_BF16 : W4A4_F16, static_cast<MX4Tile>(way - kFew), st);
+    }
 }
 
 }  // namespace
@@ -119,6 +142,7 @@ extern "C" int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void 
     if (A->rows == 0) return W4A4_OK;
     if (!out) return W4A4_ERR_INVALID_ARG;
     if (W->rows % 8 || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    const LinearArgs a{A->q, W->q, A->scale, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), A->rows, W->rows, mx4_planes(A->K), act, 0};
+    if (((long)A->rows / 16 + 1) * ((long)W->rows / 16 + 1) > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;    // (of the smallest tiles: a grid)
+    const MX4LinearArgs a{A->q, W->q, A->scale, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), A->rows, W->rows, mx4_planes(A->K), act, 0, 0, 0};
     return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
 }
