@@ -1020,10 +1020,15 @@ class _PreparedOn(_Prepared):
         self.device = next(iter(devices))
 
     def __call__(self, stream=None):
-        if torch.cuda.current_device() == self.device.index:
-            return super().__call__(stream)
-        with torch.cuda.device(self.device):
-            return super().__call__(stream)
+        now = torch.cuda.current_device()
+        if now != self.device.index:
+            with torch.cuda.device(self.device):
+                return self(stream)
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(now)
+        rc = self.fn(self.call_ref, stream)
+        if rc:
+            raise W4A4Error(rc, self.name)
 
 
 def rotary_frequencies(pairs: int, base=10000.0, factor=1.0, trained=0, slow=1.0, fast=32.0):

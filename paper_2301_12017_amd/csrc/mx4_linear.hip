@@ -77,7 +77,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
 #pragma unroll
         for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
         const float bias = a.bias ? to_float<BF16>(a.bias[n0 + n]) : 0.0f;
-        a.out[(size_t)(m0 + m) * a.N + n0 + n] = from_float<BF16>(a.act == W4A4_ACT_GELU ? mx4_finish<true>(y, bias) : mx4_finish<false>(y, bias));
+        a.out[(size_t)(m0 + m) * a.N + n0 + n] = mx4_result<BF16>(y + bias, a.act == W4A4_ACT_GELU);
     }
 }
 

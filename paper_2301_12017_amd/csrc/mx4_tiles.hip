@@ -29,17 +29,6 @@ __device__ __forceinline__ int row_at(int place) { return place % (16 / F) * F +
 template <int F>
 __device__ __forceinline__ int turn_of_row(int r, int b) { return F == 4 ? b & 3 : F == 2 ? ((r / 2) >> 2) + 2 * (b & 1) : r >> 2; }
 
-// GELU of two sums as 16-bit numbers (finite ones; the caller sees to the others).
-template <bool BF16>
-__device__ __forceinline__ uint32_t gelu2(float a, float b) {
-    if constexpr (BF16) {
-        const GeluTail p = gelu_tail_f16(a), q = gelu_tail_f16(b); // (its error, 9e-5 of the value, is a twentieth of half a step of bf16)
-        return from_float<true>(__fmaf_rn(-fabsf(a), p.p, p.relu)) | (uint32_t)from_float<true>(__fmaf_rn(-fabsf(b), q.p, q.relu)) << 16;
-    } else {
-        return gelu_erf_half2(a, b);
-    }
-}
-
 // One tile from (m0, n0) on: WM x WN waves of FM x FN fragments, KS times that with every KS-th plane each; a ring of NS steps.
 template <int FM, int FN, int WM, int WN, int KS, int NS, bool BF16>
 __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int m0, int n0) {
@@ -226,7 +215,7 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
 #pragma unroll
         for (int j = 0; j < FN; j += 2) {
             finite = __fmaf_rn(y[j], 0.0f, __fmaf_rn(y[j + 1], 0.0f, finite));
-            w[j / 2] = gelu2<BF16>(y[j], y[j + 1]);
+            w[j / 2] = mx4_gelu2<BF16>(y[j], y[j + 1]);
         }
         store_words<FN / 2, kStreamed>(out, at, w);
     });
@@ -234,9 +223,9 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
     results([&](uint32_t at, float (&y)[FN]) {
 #pragma unroll
         for (int j = 0; j < FN; j += 2) {
-            w[j / 2] = gelu2<BF16>(y[j], y[j + 1]);
-            if (!(fabsf(y[j]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFF0000u) | from_float<BF16>(mx4_finish<true>(y[j], 0.0f));
-            if (!(fabsf(y[j + 1]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFFu) | (uint32_t)from_float<BF16>(mx4_finish<true>(y[j + 1], 0.0f)) << 16;
+            w[j / 2] = mx4_gelu2<BF16>(y[j], y[j + 1]);
+            if (!(fabsf(y[j]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFF0000u) | from_float<BF16>(mx4_gelu_limit(y[j]));
+            if (!(fabsf(y[j + 1]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFFu) | (uint32_t)from_float<BF16>(mx4_gelu_limit(y[j + 1])) << 16;
         }
         store_words<FN / 2, kStreamed>(out, at, w);
     });

@@ -168,10 +168,13 @@ def _exact_operand(g, rows, K):
 
 SIZES = [(1, 8, 32), (1, 24, 128), (2, 264, 96), (5, 1024, 1056), (16, 136, 288), (17, 72, 512), (33, 520, 160), (48, 40, 4096), (64, 256, 256), (65, 128, 640),
          (127, 136, 384), (130, 264, 1056), (200, 1000, 512), (256, 256, 128), (257, 520, 1184), (300, 4096, 96), (515, 768, 800), (1031, 264, 2080), (2050, 1544, 288)]
+# the kinds of tiles in LDS, two sizes of each: 64 x 64, 64 x 128, 128 x 128, 128 x 256, 256 x 256 (the last two with tiles taken in quarters)
+TILES = [(300, 2056, 1056), (330, 2120, 1184), (257, 2056, 32), (300, 4168, 672), (1000, 4104, 288), (200, 12296, 32), (700, 8200, 160), (777, 8328, 224), (5001, 2056, 96),
+         (4300, 4104, 160), (4609, 3848, 544)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("M,N,K", SIZES + TILES)
 def test_linear_exact(B, M, N, K, dtype):
     """Products are multiples of 1/4 below 2^10: sums of up to 4096 of them fit 24 bits."""
     g, t = _gen(M + N + K), TYPES[dtype]
@@ -239,16 +242,36 @@ def test_linear_blocks_that_are_nan(B, M, gelu, dtype):
     assert got[bad].isnan().all() and torch.equal(got[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", TILES)
+def test_kinds_of_tiles_agree(B, M, N, K, dtype):
+    """With a bias, GELU and blocks that are NaN: the bits that few rows at a time give (their sums are exact, and GELU is one function)."""
+    g, t = _gen(M + K), TYPES[dtype]
+    a, w = _exact_operand(g, M, K), _exact_operand(g, N, K)
+    a[1][M // 2, 0] = w[1][N // 3, 0] = 255
+    a[1][:, 0] = torch.where(a[1][:, 0] == 255, 255, 122)         # (smaller sums, where GELU is more than max(x, 0))
+    if K > 32:
+        a[1][:, 1:] = 121
+    b = torch.randint(-8, 9, (N,), generator=g).to(t).cuda()
+    W = _operand(B, *w)
+    got = B.mx4_linear(_operand(B, *a), W, b, B.ACT_GELU, t).cpu()
+    rows = sorted({0, 1, 31, 64, M // 2, M // 2 + 1, M - 66, M - 33, M - 2, M - 1})
+    few = B.mx4_linear(_operand(B, a[0][rows], a[1][rows]), W, b, B.ACT_GELU, t).cpu()
+    assert torch.equal(got[rows].view(torch.int16)[~few.isnan()], few.view(torch.int16)[~few.isnan()])
+    assert torch.equal(got[rows].isnan(), few.isnan()) and got[M // 2].isnan().all() and got[:, N // 3].isnan().all() and got.isnan().sum() == M + N - 1
+
+
 def test_linear_past_the_largest_number(B):
     """Sums past fp32 and past fp16 are infinities, GELU of them too; far below zero it is 0."""
-    for M in (2, 70, 400):
+    for M, N in ((2, 16), (70, 16), (400, 16), (300, 2056), (1000, 4104)):
         a = torch.full((M, 32), 7), torch.full((M, 1), 254)
-        w = torch.full((16, 32), 7), torch.full((16, 1), 254)
+        w = torch.full((N, 32), 7), torch.full((N, 1), 254)
         w[0][1] = 15
         got = B.mx4_linear(_operand(B, *a), _operand(B, *w), dtype=torch.bfloat16).cpu()
         assert (got[:, 0] == float("inf")).all() and (got[:, 1] == -float("inf")).all()
-        got = B.mx4_linear(_operand(B, *a), _operand(B, *w), None, B.ACT_GELU).cpu()
-        assert (got[:, 0] == float("inf")).all() and (got[:, 1] == 0).all()
+        for t in TYPES.values():
+            got = B.mx4_linear(_operand(B, *a), _operand(B, *w), None, B.ACT_GELU, t).cpu()
+            assert (got[:, 0] == float("inf")).all() and (got[:, 1] == 0).all()
         a[1][:], w[1][:] = 134, 134
         got = B.mx4_linear(_operand(B, *a), _operand(B, *w)).cpu()
         assert (got[:, 0] == float("inf")).all() and (got[:, 1] == -float("inf")).all()
