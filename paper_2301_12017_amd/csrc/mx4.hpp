@@ -42,6 +42,25 @@ __device__ __forceinline__ uint16_t mx4_result(float y, bool gelu) {
     return fabsf(y) < INFINITY ? (uint16_t)mx4_gelu2<BF16>(y, y) : from_float<BF16>(mx4_gelu_limit(y));
 }
 
+// Tiles of a product.  A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us
+// by tiles of one kind: small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s, whatever is asked for at once), large ones
+// bring less in all.
+struct MX4Way {
+    int bm, bn;
+    float start, plane, more, tile;
+};
+inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int cus) {
+    int best = 0;
+    float least = INFINITY;
+    for (int i = 0; i < count; ++i) {
+        const MX4Way &w = ways[i];
+        const float tiles = (float)(((long)M + w.bm - 1) / w.bm) * (float)(((long)N + w.bn - 1) / w.bn), rest = tiles / (float)cus - 1.0f;
+        const float us = w.start + w.plane * (float)planes + (rest > 0.0f ? (w.more * (float)planes + w.tile) * rest : 0.0f);
+        if (us < least) least = us, best = i;
+    }
+    return best;
+}
+
 // W4A4_OK, or what is wrong with an operand.
 inline int mx4_check(const w4a4_mx4 *Q) {
     if (!Q || Q->rows < 0 || Q->K <= 0) return W4A4_ERR_INVALID_ARG;

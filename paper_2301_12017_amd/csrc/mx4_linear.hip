@@ -81,30 +81,11 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
     }
 }
 
-// A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us by tiles of one kind:
-// small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s of them, whatever is asked for at once), large ones bring less
-// in all.  The constants are fitted to 100 to 110 sizes of 1 to 16538 tokens; over 150 sizes the choice is 3 % above the best of fourteen kinds, 27 % at worst.
-struct Way {
-    int bm, bn;
-    float start, plane, more, tile;
-};
-constexpr int kFew = 3;                                            // the first of them are this file's, the others kMX4Tile..
-constexpr Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f},   {32, 32, 2.35f, 0.069f, 0.074f, 0.705f},
-                         {64, 64, 4.14f, 0.096f, 0.132f, 2.735f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f},
-                         {128, 256, 4.14f, 0.413f, 0.587f, 3.836f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f}};
-
-int way_of(const MX4LinearArgs &a, int cus) {
-    int best = 0;
-    float least = INFINITY;
-    const int ways = a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew;      // (the tiles in LDS have 32-bit offsets into the results)
-    for (int i = 0; i < ways; ++i) {
-        const Way &w = kWays[i];
-        const float tiles = (float)(((long)a.M + w.bm - 1) / w.bm) * (float)(((long)a.N + w.bn - 1) / w.bn), rest = tiles / (float)cus - 1.0f;
-        const float us = w.start + w.plane * (float)a.planes + (rest > 0.0f ? (w.more * (float)a.planes + w.tile) * rest : 0.0f);
-        if (us < least) least = us, best = i;
-    }
-    return best;
-}
+// The constants are fitted to 100 to 110 sizes of 1 to 16538 tokens; over 150 sizes the choice is 3 % above the best of fourteen kinds, 27 % at worst.
+constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
+constexpr MX4Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f},   {32, 32, 2.35f, 0.069f, 0.074f, 0.705f},
+                            {64, 64, 4.14f, 0.096f, 0.132f, 2.735f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f},
+                            {128, 256, 4.14f, 0.413f, 0.587f, 3.836f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f}};
 
 template <bool BF16, int MT, int NT, int NW>
 int launch_few(MX4LinearArgs a, hipStream_t st) {
@@ -121,7 +102,8 @@ int pick(const MX4LinearArgs &a, hipStream_t st) {
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_few_kernel<BF16, 1, 1, 8>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
-    const int way = way_of(a, cus);
+    // (the tiles in LDS have 32-bit offsets into a row of tiles' results)
+    const int way = mx4_way(kWays, a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew, a.M, a.N, a.planes, cus);
     switch (way) {
         case 0: return launch_few<BF16, 1, 1, 8>(a, st);
         case 1: return launch_few<BF16, 1, 2, 8>(a, st);

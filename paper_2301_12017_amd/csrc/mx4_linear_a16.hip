@@ -6,21 +6,18 @@
 // at a time and exact (the exponents stay out: they pass what fp16 holds); 32 of them are one matrix instruction, whose sums in
 // fp32 go into the total with the block's power of two.
 //
-// A wave reads a plane of 16 channels as one kilobyte: a lane has a block, four words of eight codes.  The four lanes that share a channel
-// change words (two lane swaps a pair), so that each instruction has one block of all 16 channels and a row of x is read 64 bytes at a time.
+// A wave has some planes of K for itself.  It reads a plane of 16 channels as one kilobyte: a lane has a block, four words of eight codes.  The four lanes
+// that share a channel change words (two lane swaps a pair), so that each instruction has one block of all 16 channels and a row of x is read 64 bytes
+// at a time.  What is on its way is held in registers, two planes of it; the waves' sums are added up in LDS, in their order.
+//
+// What bounds it is what a CU takes in, some 65 GB/s: its channels' codes and all of x.  16 tokens 264 x 5504 take 6.9 us, 3.9 without the loads of x;
+// leaving out conversion, exponents or products changes 2 to 7 %.  Three or four planes on their way instead of two, and DMA into LDS instead of
+// registers, were no faster.
+#include "gemm_common.hpp"
 #include "mx4.hpp"
 
 namespace w4a4 {
 namespace {
-
-struct A16Args {
-    const uint16_t *x;
-    const uint8_t *w;
-    const uint32_t *sw;
-    const uint16_t *bias;
-    uint16_t *out;
-    int M, N, K, ldx, act, tiles_n;
-};
 
 // words (lane group g, j) -> (lane group j, word g) for the four groups of sixteen lanes
 __device__ __forceinline__ u32x4_t transpose_groups(u32x4_t w) {
@@ -30,6 +27,15 @@ __device__ __forceinline__ u32x4_t transpose_groups(u32x4_t w) {
     const auto d = __builtin_amdgcn_permlane16_swap((unsigned)a[1], (unsigned)b[1], false, false);
     return u32x4_t{(unsigned)c[0], (unsigned)c[1], (unsigned)d[0], (unsigned)d[1]};
 }
+
+struct A16Args {
+    const uint16_t *x;
+    const uint8_t *w;
+    const uint32_t *sw;
+    const uint16_t *bias;
+    uint16_t *out;
+    int M, N, K, ldx, act, tiles_n;
+};
 
 template <bool BF16>
 __device__ __forceinline__ u32x4_t numbers8(uint32_t w) {          // eight codes as 16-bit numbers
@@ -42,49 +48,56 @@ __device__ __forceinline__ u32x4_t numbers8(uint32_t w) {          // eight code
     return o;
 }
 
-template <bool BF16, int MT, int NT, int NW>
-__global__ __launch_bounds__(NW * 64) void mx4_linear_a16_kernel(A16Args a) {
+template <bool BF16, int MT, int NT, int NW, int AHEAD>
+__global__ __launch_bounds__(NW * 64, NW / 4) void mx4_linear_a16_kernel(A16Args a) {
     extern __shared__ float red[];                                 // [NW][MT * NT * 4][64]
-    constexpr int AHEAD = 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
     const int m0 = blockIdx.x / a.tiles_n * (16 * MT), n0 = blockIdx.x % a.tiles_n * (16 * NT);
     const int planes = (a.K + kPlane - 1) / kPlane, each = (planes + NW - 1) / NW, c0 = wave * each, c1 = min(c0 + each, planes);
     struct Stage {
-        u32x4_t w[NT];
+        u32x4_t w[NT], x[MT][4];
         uint32_t s[NT];
     } st[AHEAD];
+    // Rows of x whose bytes at the same place lie in the same half of a cache line are read in turn, one its first 64 bytes of 128, the next its second
+    // ones.  (All rows of a lane are alike: sixteen rows are a multiple of 128 bytes.)
+    const int half = ((uint32_t)((reinterpret_cast<uintptr_t>(a.x) + (size_t)(m0 + col) * a.ldx * 2) >> 6) ^ (uint32_t)col) & 1 ? 32 : 0;
+    // Everything comes through descriptors, outside of which zeros are read: rows of x behind the last one, their numbers behind K, planes of other waves.
+    // (Loads under a condition would be waited for at once, where the two ways meet.)
+    const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x + (size_t)m0 * a.ldx, (uint32_t)(((long)min(16 * MT, a.M - m0) - 1) * a.ldx + a.K) * 2);
+    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
+    int xo[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xo[t] = 16 * t + col < rows ? ((16 * t + col) * a.ldx + 8 * kg) * 2 : (int)kPoison;
     auto load = [&](Stage &s, int c) {
+        const size_t at = (size_t)c * a.N + n0;
+        const __amdgpu_buffer_rsrc_t w = make_rsrc(a.w + at * kPlaneBytes, c < c1 ? (uint32_t)cols * kPlaneBytes : 0), e = make_rsrc(a.sw + at, c < c1 ? (uint32_t)cols * 4 : 0);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const size_t at = (size_t)c * a.N + min(n0 + 16 * t + col, a.N - 1);
-            s.w[t] = *reinterpret_cast<const u32x4_t *>(a.w + at * kPlaneBytes + 16 * kg);
-            s.s[t] = a.sw[at];
+            s.w[t] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(w, (16 * t + col) * kPlaneBytes + 16 * kg, 0, 0));
+            s.s[t] = __builtin_amdgcn_raw_buffer_load_b32(e, (16 * t + col) * 4, 0, 0);
         }
-    };
-    u32x4_t x[MT][4];
-    auto load_x = [&](int c) {
+        const int left = c < c1 ? a.K - c * kPlane : 0;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const uint16_t *p = a.x + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.ldx + c * kPlane + 8 * kg;
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                x[t][j] = u32x4_t{0, 0, 0, 0};
-                if (c * kPlane + 32 * j < a.K) x[t][j] = *reinterpret_cast<const u32x4_t *>(p + 32 * j);
+                const int k = 32 * j ^ half;
+                s.x[t][j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(xr, k < left ? xo[t] + (c * kPlane + k) * 2 : (int)kPoison, 0, 0));
             }
-        }
     };
     float4_t tot[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) tot[i][t] = float4_t{0, 0, 0, 0};
-    auto compute = [&](Stage &s, int next) {
-        u32x4_t xr[MT][4];
+    auto compute = [&](const Stage &s) {
+        u32x4_t x[MT][4];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xr[i][j] = x[i][j];
-        if (next < c1) load_x(next);
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][j][e] = half ? s.x[i][j ^ 1][e] : s.x[i][j][e];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const u32x4_t w4 = transpose_groups(s.w[t]);
@@ -94,24 +107,22 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_a16_kernel(A16Args a) {
                 const float by = mx4_scale(s.s[t] >> (8 * j) & 255);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const float4_t sum = mfma16<BF16>(xr[i][j], w, float4_t{0, 0, 0, 0});
+                    const float4_t sum = mfma16<BF16>(x[i][j], w, float4_t{0, 0, 0, 0});
 #pragma unroll
                     for (int e = 0; e < 4; ++e) tot[i][t][e] = __fmaf_rn(sum[e], by, tot[i][t][e]);
                 }
             }
+            if (NT > 1) __builtin_amdgcn_sched_barrier(0);
         }
     };
     if (c0 < c1) {
 #pragma unroll
-        for (int p = 0; p < AHEAD; ++p)
-            if (c0 + p < c1) load(st[p], c0 + p);
-        load_x(c0);
+        for (int p = 0; p < AHEAD; ++p) load(st[p], c0 + p);
         for (int c = c0; c < c1; c += AHEAD) {
 #pragma unroll
             for (int p = 0; p < AHEAD; ++p) {
-                if (c + p >= c1) break;
-                compute(st[p], c + p + 1);
-                if (c + p + AHEAD < c1) load(st[p], c + p + AHEAD);
+                if (p == 0 || c + p < c1) compute(st[p]);
+                load(st[p], c + p + AHEAD);                        // (zeros behind the last one)
             }
         }
     }
@@ -123,7 +134,6 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_a16_kernel(A16Args a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) red[(wave * REGS + (i * NT + t) * 4 + e) * 64 + lane] = tot[i][t][e];
     __syncthreads();
-    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
     for (int o = threadIdx.x; o < rows * 16 * NT; o += NW * 64) {
         const int m = o / (16 * NT), n = o % (16 * NT);
         if (n >= cols) continue;
@@ -136,23 +146,33 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_a16_kernel(A16Args a) {
     }
 }
 
-template <bool BF16, int MT, int NT, int NW>
+template <bool BF16, int MT, int NT>
 int launch(A16Args a, hipStream_t st) {
-    auto kern = mx4_linear_a16_kernel<BF16, MT, NT, NW>;
+    constexpr int NW = 8;
+    auto kern = mx4_linear_a16_kernel<BF16, MT, NT, NW, 2>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
     const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
-    if (tiles > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
     static KernelState ks;
     if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
     return launch_status();
 }
 
+// Fitted to 110 sizes of 1 to 64 tokens, over which the choice is 1 % above the best of the four, 25 % at worst.
+constexpr MX4Way kWays[] = {{16, 16, 2.48f, 0.106f, 0.087f, 0.655f}, {16, 32, 2.65f, 0.155f, 0.128f, 1.403f}, {32, 32, 3.22f, 0.272f, 0.195f, 5.505f}, {32, 64, 3.60f, 0.396f, 0.270f, 0.495f}};
+
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
-    if (a.M <= 16) return launch<BF16, 1, 1, 8>(a, st);
-    return launch<BF16, 2, 1, 8>(a, st);
+    static KernelState ks;
+    const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_a16_kernel<BF16, 1, 1, 8, 2>), 0, ks);
+    if (cus < 0) return W4A4_ERR_HIP;
+    switch (mx4_way(kWays, 4, a.M, a.N, mx4_planes(a.K), cus)) {
+        case 0: return launch<BF16, 1, 1>(a, st);
+        case 1: return launch<BF16, 1, 2>(a, st);
+        case 2: return launch<BF16, 2, 2>(a, st);
+        default: return launch<BF16, 2, 4>(a, st);
+    }
 }
 
 }  // namespace
@@ -165,7 +185,8 @@ extern "C" int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, con
     if (M < 0 || ldx < W->K || W->rows == 0 || (dtype != W4A4_F16 && dtype != W4A4_BF16) || (act != W4A4_ACT_NONE && act != W4A4_ACT_GELU)) return W4A4_ERR_INVALID_ARG;
     if (M == 0) return W4A4_OK;
     if (!X || !out) return W4A4_ERR_INVALID_ARG;
-    if (W->rows % 8 || ldx % 8 || !aligned16(X) || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    if (W->rows % 8 || ldx % 8 || ldx >= 1 << 24 || !aligned16(X) || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    if (((long)M / 16 + 1) * ((long)W->rows / 16 + 1) > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;          // (of the smallest tiles: a grid)
     const A16Args a{static_cast<const uint16_t *>(X), W->q, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), M, W->rows, W->K, ldx, act, 0};
     return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
 }

@@ -71,7 +71,7 @@ def test_mx4_linear_a16_refusals(b):
         assert f(W=c) == rc
     assert f(M=-1) == -1 and f(ldx=56) == -1 and f(dtype=2) == -1 and f(act=-1) == -1 and f(W=_mx4(b, rows=0)) == -1 and f(X=None) == -1 and f(out=None) == -1
     assert f(W=_mx4(b, rows=12)) == -2 and f(ldx=68) == -2 and f(X=P + 4) == -2 and f(out=P + 8) == -2 and f(bias=P + 4) == -2
-    assert f(M=BIG, W=_mx4(b, rows=BIG - 7)) == -2
+    assert f(M=BIG, W=_mx4(b, rows=BIG - 7)) == -2 and f(ldx=1 << 24) == -2
     assert f(M=0, X=None, out=None) == 0
 
 
