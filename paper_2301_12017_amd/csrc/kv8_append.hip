@@ -20,6 +20,8 @@
 namespace w4a4 {
 namespace {
 
+enum Positions { kNone, kKeys, kKeysAndQueries };                   // what turns on the way
+
 constexpr int kPiece = 16;                                         // tokens of a run that a wave takes at once
 
 struct AppendArgs {
@@ -31,6 +33,7 @@ struct AppendArgs {
     int T, blocks, H, shift, tile;
     const int32_t *positions;                                      // keys that turn
     RotaryArgs r;
+    RotaryWork q;                                                  // the step's queries
 };
 
 // Code of x.  CAREFUL, where infinities or NaN are among the tokens: NaN is stored as 0, an infinity as +-127.  Else |x| is at most
@@ -92,58 +95,64 @@ __device__ __forceinline__ float settle(float *scale, float had, int8_t *codes, 
     return now > 0.0f ? 1.0f / now : 0.0f;
 }
 
-// The features d .. d+7 of a key x (a lane's, in w) turned by its token's position.
+// The features d .. d+7 of a key (a lane's, in w), turned: `other` holds their partners where pairs are halves, cosines and sines of the token's pairs lie in LDS.
 template <bool BF16>
-__device__ __forceinline__ void turn8(const RotaryArgs &r, const uint16_t *x, u32x4_t w, int d, int position, float (&to)[8]) {
+__device__ __forceinline__ void turn8(const RotaryArgs &r, u32x4_t w, u32x4_t other, int d, const float *cosines, const float *sines, float (&to)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) to[j] = to_float<BF16>((uint16_t)(w[j / 2] >> (16 * (j % 2))));
-    if (position < 0) return;
     if (r.interleaved) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             const int p = (d + j) / 2;
             if (p >= r.pairs) break;
-            const Turn t = turn_of(r.turns[p], (uint32_t)position, r.magnitude, r.inverse);
+            const Turn t{cosines[p], sines[p]};
             const float u = to[j], v = to[j + 1];
             to[j] = turned_a(t, u, v);
             to[j + 1] = turned_b(t, u, v);
         }
         return;
     }
-    if (d >= 2 * r.pairs) return;
-    uint32_t other[4];                                             // the partners: of halves that are whole pieces sixteen bytes
-    if (r.pairs % 8 == 0) {
-        const u32x4_t o = *reinterpret_cast<const u32x4_t *>(d < r.pairs ? x + r.pairs : x - r.pairs);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) other[j] = o[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            uint32_t o[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int f = d + j + e;
-                o[e] = x[f < r.pairs ? j + e + r.pairs : f < 2 * r.pairs ? j + e - r.pairs : j + e];
-            }
-            other[j / 2] = o[0] | o[1] << 16;
-        }
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int f = d + j;
+        const int f = d + j, p = f < r.pairs ? f : f - r.pairs;
         if (f >= 2 * r.pairs) break;
-        const Turn t = turn_of(r.turns[f < r.pairs ? f : f - r.pairs], (uint32_t)position, r.magnitude, r.inverse);
+        const Turn t{cosines[p], sines[p]};
         const float v = to_float<BF16>((uint16_t)(other[j / 2] >> (16 * (j % 2))));
         to[j] = f < r.pairs ? turned_a(t, to[j], v) : turned_b(t, v, to[j]);
     }
 }
 
+// Cosines and sines of the pairs of kWindow tokens from `first` on, and those tokens' positions, in LDS: found by all four waves of a workgroup together.
+constexpr int kWindow = 32;
+struct Window {
+    float *cosines, *sines;                                        // [kWindow][pairs]
+    int *positions;                                                // [kWindow]
+    int first, count;
+    __device__ __forceinline__ void fill(const AppendArgs &a, int from, int tokens) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.r.pairs;
+        first = from;
+        count = min(tokens, a.T - from);
+        if ((int)threadIdx.x < count) positions[threadIdx.x] = a.positions[from + threadIdx.x];
+        for (int p = lane; p < pairs; p += 64) {
+            const uint64_t per = a.r.turns[p];
+            for (int t = wave; t < count; t += 4) {
+                const Turn turn = turn_of(per, (uint32_t)a.positions[from + t], a.r.magnitude, a.r.inverse);
+                cosines[t * pairs + p] = turn.cos;
+                sines[t * pairs + p] = turn.sin;
+            }
+        }
+    }
+};
+
 // Keys: tokens t0 .. t1-1 into the block's rows.
+// ROTARY: the four waves of a workgroup have four heads (h past the last one: nothing) and do the same steps, and find the angles together.
 template <bool BF16, int D, bool ROTARY>
-__device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane) {
+__device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane, Window &window) {
     constexpr int LANES = D / 8, ROWS = 64 / LANES, N = (kPiece + ROWS - 1) / ROWS;   // lanes of a row, rows at once, loads of a chunk
     const int block = 1 << a.shift, row = lane / LANES;
-    const bool on = row < ROWS;
+    const bool there = !ROTARY || h < a.H;
+    const bool on = row < ROWS && there;
+    if (!there) h = 0;
     const uint16_t *x = a.x[0] + h * D + lane % LANES * 8;
     const size_t unit = (size_t)b * a.H + h;
     int8_t *codes = a.k + unit * D * block;
@@ -157,21 +166,55 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
             w[i] = u32x4_t{0, 0, 0, 0};
             if (on && t < t1) w[i] = *reinterpret_cast<const u32x4_t *>(x + t * a.ld[0]);
         }
-        if constexpr (ROTARY)
+    };
+    auto load_turned = [&](int c) {
+        const int pairs = a.r.pairs, d = lane % LANES * 8;
+        u32x4_t other[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int t = c + i * ROWS + row;
-                if (on && t < t1) turn8<BF16>(a.r, x + t * a.ld[0], w[i], lane % LANES * 8, a.positions[t], turned[i]);
-                else
+        for (int i = 0; i < N; ++i) {                              // (rows that are not there: the last one again)
+            const uint16_t *p = x + min(c + i * ROWS + min(row, ROWS - 1), t1 - 1) * a.ld[0];
+            w[i] = *reinterpret_cast<const u32x4_t *>(p);
+            if (a.r.interleaved || d >= 2 * pairs) continue;
+            if (pairs % 8 == 0) {
+                other[i] = *reinterpret_cast<const u32x4_t *>(d < pairs ? p + pairs : p - pairs);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) turned[i][j] = 0.0f;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t o[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int f = d + 2 * j + e;
+                        o[e] = p[f < pairs ? 2 * j + e + pairs : f < 2 * pairs ? 2 * j + e - pairs : 2 * j + e];
+                    }
+                    other[i][j] = o[0] | o[1] << 16;
+                }
             }
+        }
+        if (c < window.first || min(c + N * ROWS, t1) > window.first + window.count) {
+            __syncthreads();                                       // (the angles before have been read)
+            window.fill(a, c, kWindow);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int t = c + i * ROWS + min(row, ROWS - 1), at = min(t, t1 - 1) - window.first;
+            if (window.positions[at] >= 0) {
+                turn8<BF16>(a.r, w[i], other[i], d, window.cosines + at * pairs, window.sines + at * pairs, turned[ROTARY ? i : 0]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) turned[ROTARY ? i : 0][j] = to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2))));
+            }
+            if (!on || t >= t1)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) turned[ROTARY ? i : 0][j] = 0.0f;
+        }
     };
     auto range = [&](bool careful) {                               // (of turned keys the bits of an fp32 number)
         Range m;
         uint32_t most = 0;
         for (int c = t0; c < t1; c += N * ROWS) {
-            load(c);
+            if constexpr (ROTARY) load_turned(c);
+            else load(c);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if constexpr (ROTARY) {
@@ -190,13 +233,20 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
         else return m.over_wave();
     };
     uint32_t wide = range(false);
-    const bool careful = wide >= (ROTARY ? 0x7F800000u : kInf<BF16>);
-    if (careful) wide = range(true);
-    const float inv = settle(a.k_scale + unit, had, codes, D * block, first, ROTARY ? __builtin_bit_cast(float, wide) : to_float<BF16>((uint16_t)wide), lane);
+    bool careful = wide >= (ROTARY ? 0x7F800000u : kInf<BF16>);
+    if (ROTARY ? __syncthreads_or(careful) : careful) {            // (all waves take the same steps)
+        const uint32_t finite = range(true);
+        if (careful) wide = finite;
+    }
+    float inv = 0.0f;
+    if (there) inv = settle(a.k_scale + unit, had, codes, D * block, first, ROTARY ? __builtin_bit_cast(float, wide) : to_float<BF16>((uint16_t)wide), lane);
     auto write = [&](auto careful) {
         constexpr bool C = decltype(careful)::value;
         for (int c = t0; c < t1; c += N * ROWS) {
-            if (t1 - t0 > N * ROWS) load(c);
+            if (t1 - t0 > N * ROWS) {
+                if constexpr (ROTARY) load_turned(c);
+                else load(c);
+            }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int t = c + i * ROWS + row;
@@ -209,7 +259,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
             }
         }
     };
-    if (careful) write(std::true_type{});
+    if (ROTARY ? __syncthreads_or(careful) : careful) write(std::true_type{});
     else write(std::false_type{});
 }
 
@@ -312,11 +362,38 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     else write(std::false_type{});
 }
 
-template <bool BF16, int D, bool ROTARY>
-__global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int which = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);   // 0 .. H-1: keys of a head, H .. 2H-1: values
-    if (which >= 2 * a.H) return;
+// (Turning keys takes registers that the values' waves would rather do without: with three waves a SIMD asked for, 10002 tokens of 8 heads of 128 take 33 us, with
+// two 39, with four, which spill, 58; without positions 20.)
+template <bool BF16, int D, Positions POSITIONS>
+__global__ __launch_bounds__(256, POSITIONS == kKeys && D <= 128 ? 3 : 1) void kv8_append_kernel(AppendArgs a) {
+    constexpr bool ROTARY = POSITIONS != kNone;
+    extern __shared__ float angles[];                              // ROTARY: a window's
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quads = (a.H + 3) / 4;
+    // 0 .. H-1: keys of a head, H .. 2H-1: values.  ROTARY: workgroups of four heads' keys, then of four heads' values, then of queries
+    int which = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);
+    bool values = which >= a.H;
+    Window window{};
+    if constexpr (ROTARY) {
+        if (POSITIONS == kKeysAndQueries && (int)blockIdx.y == 2 * quads) {
+            switch (a.q.way) {
+                case kRotaryNeighbours: return rotary_tokens<BF16, kRotaryNeighbours, 1>(a.q, blockIdx.x, 1);
+                case kRotaryHalves8: return rotary_tokens<BF16, kRotaryHalves8, 1>(a.q, blockIdx.x, 1);
+                case kRotaryHalves4: return rotary_tokens<BF16, kRotaryHalves4, 1>(a.q, blockIdx.x, 1);
+                default: return rotary_tokens<BF16, kRotarySingle, 1>(a.q, blockIdx.x, 1);
+            }
+        }
+        values = (int)blockIdx.y >= quads;
+        which = __builtin_amdgcn_readfirstlane((blockIdx.y - (values ? quads : 0)) * 4 + wave);
+        if (values && which >= a.H) return;
+        window = Window{angles, angles + kWindow * a.r.pairs, reinterpret_cast<int *>(angles + 2 * kWindow * a.r.pairs), 0, 0};
+        if (!values) {
+            window.fill(a, blockIdx.x * a.tile, a.tile == 1 ? 1 : kWindow);
+            __syncthreads();
+        }
+    } else {
+        if (which >= 2 * a.H) return;
+        if (values) which -= a.H;
+    }
     const int t_first = blockIdx.x * a.tile, t_last = min(t_first + a.tile, a.T), mask = (1 << a.shift) - 1;
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> a.shift) < a.blocks ? slot >> a.shift : -1; };   // -1: not stored
     // slots of the token before the tile and of the 63 from its first one on; where runs begin; where a slot does not follow the one before
@@ -350,8 +427,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
             }
         }
         const int off = __builtin_amdgcn_readlane(slot, i) & mask;
-        if (which < a.H) append_keys<BF16, D, ROTARY>(a, t0, t1, bi, which, first, lane);
-        else append_values<BF16, D>(a, t0, t1, bi, which - a.H, first, ordered, off, lane);
+        if (!values) append_keys<BF16, D, ROTARY>(a, t0, t1, bi, which, first, lane, window);
+        else append_values<BF16, D>(a, t0, t1, bi, which, first, ordered, off, lane);
     }
 }
 
@@ -506,16 +583,22 @@ int rows_check(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype,
     return W4A4_OK;
 }
 
-template <bool ROTARY>
+// Up to this many tokens a workgroup has one of them, and the queries turn in the same launch.  (Behind it, where memory is what counts, queries have a launch
+// of their own: their registers would leave the keys half as many waves.)
+constexpr int kFewTokens = 512;
+
+template <Positions POSITIONS>
 int append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv, const int32_t *slots, const int32_t *positions,
-           const RotaryArgs &r, hipStream_t st) {
+           const RotaryArgs &r, const RotaryWork &q, hipStream_t st) {
     AppendArgs a{C->k, C->v, C->k_scale, C->v_scale, {static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V)}, {ldk, ldv},
-                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece, positions, r};
-    const dim3 grid((tokens + a.tile - 1) / a.tile, (2 * C->heads + 3) / 4);
+                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= kFewTokens ? 1 : kPiece, positions, r, q};
+    const dim3 grid((tokens + a.tile - 1) / a.tile, POSITIONS == kNone ? (2 * C->heads + 3) / 4 : 2 * ((C->heads + 3) / 4) + (POSITIONS == kKeysAndQueries));
     return by_features(C->features, [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (dtype == W4A4_BF16) hipLaunchKernelGGL((kv8_append_kernel<true, D, ROTARY>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((kv8_append_kernel<false, D, ROTARY>), grid, dim3(256), 0, st, a);
+        static_assert((kPiece + 64 / (D / 8) - 1) / (64 / (D / 8)) * (64 / (D / 8)) <= kWindow, "a chunk of rows has its angles in one window");
+        const size_t lds = POSITIONS != kNone ? (size_t)kWindow * (2 * r.pairs + 1) * sizeof(float) : 0;          // at most 33 KB
+        if (dtype == W4A4_BF16) hipLaunchKernelGGL((kv8_append_kernel<true, D, POSITIONS>), grid, dim3(256), lds, st, a);
+        else hipLaunchKernelGGL((kv8_append_kernel<false, D, POSITIONS>), grid, dim3(256), lds, st, a);
         return launch_status();
     });
 }
@@ -526,7 +609,7 @@ extern "C" int w4a4_kv8_append(const w4a4_kv8_cache *C, const void *K, const voi
                                const int32_t *slots, void *stream) {
     if (const int rc = rows_check(C, K, V, dtype, tokens, ldk, ldv, slots)) return rc;
     if (tokens == 0) return W4A4_OK;
-    return append<false>(C, K, V, dtype, tokens, ldk, ldv, slots, nullptr, RotaryArgs{}, as_stream(stream));
+    return append<kNone>(C, K, V, dtype, tokens, ldk, ldv, slots, nullptr, RotaryArgs{}, RotaryWork{}, as_stream(stream));
 }
 
 extern "C" int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_rows *T, const w4a4_rotary_angles *R, void *stream) {
@@ -538,9 +621,14 @@ extern "C" int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_ro
     if (!T->positions || !T->q != !T->q_out || (T->q && T->q == T->q_out)) return W4A4_ERR_INVALID_ARG;
     if (T->q && (T->ldq % 8 || !aligned16(T->q) || !aligned16(T->q_out))) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const RotaryArgs r = rotary_args(R);
-    if (const int rc = append<true>(C, T->k, T->v, T->dtype, T->tokens, T->ldk, T->ldv, T->slots, T->positions, r, as_stream(stream))) return rc;
-    if (!T->q) return W4A4_OK;
-    return rotary_launch(T->q, T->dtype, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, as_stream(stream));
+    hipStream_t st = as_stream(stream);
+    auto keys = [&](auto positions, const RotaryWork &q) {
+        return append<decltype(positions)::value>(C, T->k, T->v, T->dtype, T->tokens, T->ldk, T->ldv, T->slots, T->positions, r, q, st);
+    };
+    auto queries = [&](int heads) { return rotary_work(T->q, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, heads); };
+    if (T->q && T->tokens <= kFewTokens) return keys(std::integral_constant<Positions, kKeysAndQueries>{}, queries(1));
+    if (const int rc = keys(std::integral_constant<Positions, kKeys>{}, RotaryWork{})) return rc;
+    return T->q ? rotary_launch(queries(4), T->dtype, 4, st) : W4A4_OK;
 }
 
 extern "C" int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream) {
