@@ -49,8 +49,9 @@ __device__ __forceinline__ uint32_t quantize8(u32x4_t w, uint32_t &byte) {
 template <bool BF16, int R>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long r0 = ((long)blockIdx.x * 4 + wave) * R;
-    const int k = blockIdx.y * 512 + lane * 8, c = k / kPlane, planes = (a.K + kPlane - 1) / kPlane;
+    const int cols = (a.K + 511) / 512;                            // workgroups of a row of them follow each other
+    const long r0 = ((long)(blockIdx.x / cols) * 4 + wave) * R;
+    const int k = blockIdx.x % cols * 512 + lane * 8, c = k / kPlane, planes = (a.K + kPlane - 1) / kPlane;
     if (r0 >= a.rows || c >= planes) return;                       // (sixteen lanes together)
     u32x4_t w[R];
 #pragma unroll
@@ -81,8 +82,9 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *q, const uint32_t *scale, int rows, int K, uint16_t *x) {
     constexpr int R = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long r0 = ((long)blockIdx.x * 4 + wave) * R;
-    const int k = blockIdx.y * 512 + lane * 8, c = k / kPlane;
+    const int cols = (K + 511) / 512;
+    const long r0 = ((long)(blockIdx.x / cols) * 4 + wave) * R;
+    const int k = blockIdx.x % cols * 512 + lane * 8, c = k / kPlane;
     if (r0 >= rows || k >= K) return;
     uint32_t codes[R], s[R];
 #pragma unroll
@@ -121,10 +123,11 @@ extern "C" int w4a4_mx4_quantize(const void *X, int dtype, int ldx, const w4a4_m
     if (ldx % 8 || !aligned16(X)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const QuantArgs a{static_cast<const uint16_t *>(X), out->q, out->scale, out->rows, out->K, ldx};
     const int cols = (a.K + 511) / 512;
-    if (cols > 65535) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const bool few = (long)a.rows * cols < 4096;
     const int per = few ? 4 : 16;                                  // rows of a workgroup
-    const dim3 grid((unsigned)(((long)a.rows + per - 1) / per), cols);
+    const long groups = ((long)a.rows + per - 1) / per * cols;
+    if (groups > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const dim3 grid((unsigned)groups);
     auto run = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, as_stream(stream), a); };
     if (dtype == W4A4_BF16) few ? run(mx4_quantize_kernel<true, 1>) : run(mx4_quantize_kernel<true, 4>);
     else few ? run(mx4_quantize_kernel<false, 1>) : run(mx4_quantize_kernel<false, 4>);
@@ -136,9 +139,9 @@ extern "C" int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *
     if (dtype != W4A4_F16 && dtype != W4A4_BF16) return W4A4_ERR_INVALID_ARG;
     if (Q->rows == 0) return W4A4_OK;
     if (!X) return W4A4_ERR_INVALID_ARG;
-    const int cols = (Q->K + 511) / 512;
-    if (!aligned16(X) || cols > 65535) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    const dim3 grid((unsigned)(((long)Q->rows + 15) / 16), cols);
+    const long groups = ((long)Q->rows + 15) / 16 * ((Q->K + 511) / 512);
+    if (!aligned16(X) || groups > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const dim3 grid((unsigned)groups);
     auto run = [&](auto kern) {
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, as_stream(stream), Q->q, Q->scale, Q->rows, Q->K, static_cast<uint16_t *>(X));
     };

@@ -41,8 +41,8 @@ def test_mx4_quantize_and_dequantize_refusals(b):
     assert quantize(dtype=2) == -1 and quantize(ldx=56) == -1 and quantize(X=None) == -1 and quantize(ldx=68) == -2 and quantize(X=P + 8) == -2
     assert dequantize(dtype=-1) == -1 and dequantize(X=None) == -1 and dequantize(X=P + 4) == -2
     assert quantize(_mx4(b, rows=0), X=None) == 0 and dequantize(_mx4(b, rows=0, q=None, scale=None), X=None) == 0
-    wide = _mx4(b, K=512 * 65536)
-    assert quantize(wide, ldx=512 * 65536) == -2 and dequantize(wide) == -2
+    large = _mx4(b, rows=BIG, K=32768)                            # more workgroups than a grid has
+    assert quantize(large, ldx=32768) == -2 and dequantize(large) == -2
 
 
 def test_mx4_linear_refusals(b):
