@@ -47,15 +47,15 @@ __device__ __forceinline__ uint16_t mx4_result(float y, bool gelu) {
 // bring less in all.
 struct MX4Way {
     int bm, bn;
-    float start, plane, more, tile;
+    float start, plane, more, tile, gelu;                          // gelu: more of `tile` where there is one
 };
-inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int cus) {
+inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int act, int cus) {
     int best = 0;
     float least = INFINITY;
     for (int i = 0; i < count; ++i) {
         const MX4Way &w = ways[i];
         const float tiles = (float)(((long)M + w.bm - 1) / w.bm) * (float)(((long)N + w.bn - 1) / w.bn), rest = tiles / (float)cus - 1.0f;
-        const float us = w.start + w.plane * (float)planes + (rest > 0.0f ? (w.more * (float)planes + w.tile) * rest : 0.0f);
+        const float us = w.start + w.plane * (float)planes + (rest > 0.0f ? (w.more * (float)planes + w.tile + (act == W4A4_ACT_GELU ? w.gelu : 0.0f)) * rest : 0.0f);
         if (us < least) least = us, best = i;
     }
     return best;

@@ -20,6 +20,9 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, kg = lane >> 4;
     const int m0 = blockIdx.x / a.tiles_n * (16 * MT), n0 = blockIdx.x % a.tiles_n * (16 * NT);
     const int each = (a.planes + NW - 1) / NW, c0 = wave * each, c1 = min(c0 + each, a.planes);
+    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
+    const int n = threadIdx.x % (16 * NT);                         // the channel of the results that the thread finishes
+    const uint16_t bias = a.bias ? a.bias[min(n0 + n, a.N - 1)] : 0;
     struct Stage {
         u32x4_t x[MT], w[NT];
         uint32_t sx[MT], sw[NT];
@@ -68,24 +71,22 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
 #pragma unroll
             for (int e = 0; e < 4; ++e) red[(wave * REGS + (i * NT + t) * 4 + e) * 64 + lane] = acc[i][t][e];
     __syncthreads();
-    const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
-    for (int o = threadIdx.x; o < rows * 16 * NT; o += NW * 64) {
-        const int m = o / (16 * NT), n = o % (16 * NT);
-        if (n >= cols) continue;
+    if (n >= cols) return;
+    for (int m = threadIdx.x / (16 * NT); m < rows; m += NW * 64 / (16 * NT)) {
         const int reg = ((m >> 4) * NT + (n >> 4)) * 4 + (m & 3), from = ((m & 15) >> 2) * 16 + (n & 15);
         float y = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
-        const float bias = a.bias ? to_float<BF16>(a.bias[n0 + n]) : 0.0f;
-        a.out[(size_t)(m0 + m) * a.N + n0 + n] = mx4_result<BF16>(y + bias, a.act == W4A4_ACT_GELU);
+        a.out[(size_t)(m0 + m) * a.N + n0 + n] = mx4_result<BF16>(y + to_float<BF16>(bias), a.act == W4A4_ACT_GELU);
     }
 }
 
 // The constants are fitted to 100 to 110 sizes of 1 to 16538 tokens; over 150 sizes the choice is 3 % above the best of fourteen kinds, 27 % at worst.
 constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
-constexpr MX4Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f},   {32, 32, 2.35f, 0.069f, 0.074f, 0.705f},
-                            {64, 64, 4.14f, 0.096f, 0.132f, 2.735f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f},
-                            {128, 256, 4.14f, 0.413f, 0.587f, 3.836f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f}};
+// (us of 16384 x 16384 x 1024 without GELU | with it, from 64 x 128 on: 267 | 291, 202 | 235, 194 | 248, 205 | 273.)
+constexpr MX4Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f, 0.0f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f, 0.0f},    {32, 32, 2.35f, 0.069f, 0.074f, 0.705f, 0.0f},
+                            {64, 64, 4.14f, 0.096f, 0.132f, 2.735f, 0.1f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f, 0.19f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f, 0.52f},
+                            {128, 256, 4.14f, 0.413f, 0.587f, 3.836f, 1.7f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f, 4.5f}};
 
 template <bool BF16, int MT, int NT, int NW>
 int launch_few(MX4LinearArgs a, hipStream_t st) {
@@ -103,7 +104,7 @@ int pick(const MX4LinearArgs &a, hipStream_t st) {
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_few_kernel<BF16, 1, 1, 8>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
     // (the tiles in LDS have 32-bit offsets into a row of tiles' results)
-    const int way = mx4_way(kWays, a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew, a.M, a.N, a.planes, cus);
+    const int way = mx4_way(kWays, a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew, a.M, a.N, a.planes, a.act, cus);
     switch (way) {
         case 0: return launch_few<BF16, 1, 1, 8>(a, st);
         case 1: return launch_few<BF16, 1, 2, 8>(a, st);

@@ -65,6 +65,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void mx4_linear_a16_kernel(A16Args
     // (Loads under a condition would be waited for at once, where the two ways meet.)
     const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x + (size_t)m0 * a.ldx, (uint32_t)(((long)min(16 * MT, a.M - m0) - 1) * a.ldx + a.K) * 2);
     const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
+    const int n = threadIdx.x % (16 * NT);                         // the channel of the results that the thread finishes
+    const uint16_t bias = __builtin_amdgcn_raw_buffer_load_b16(make_rsrc(a.bias, a.bias ? (uint32_t)a.N * 2 : 0), (n0 + n) * 2, 0, 0);
     int xo[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) xo[t] = 16 * t + col < rows ? ((16 * t + col) * a.ldx + 8 * kg) * 2 : (int)kPoison;
@@ -134,15 +136,13 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void mx4_linear_a16_kernel(A16Args
 #pragma unroll
             for (int e = 0; e < 4; ++e) red[(wave * REGS + (i * NT + t) * 4 + e) * 64 + lane] = tot[i][t][e];
     __syncthreads();
-    for (int o = threadIdx.x; o < rows * 16 * NT; o += NW * 64) {
-        const int m = o / (16 * NT), n = o % (16 * NT);
-        if (n >= cols) continue;
+    if (n >= cols) return;
+    for (int m = threadIdx.x / (16 * NT); m < rows; m += NW * 64 / (16 * NT)) {
         const int reg = ((m >> 4) * NT + (n >> 4)) * 4 + (m & 3), from = ((m & 15) >> 2) * 16 + (n & 15);
         float y = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) y += red[(w * REGS + reg) * 64 + from];
-        const float bias = a.bias ? to_float<BF16>(a.bias[n0 + n]) : 0.0f;
-        a.out[(size_t)(m0 + m) * a.N + n0 + n] = mx4_result<BF16>(y + bias, a.act == W4A4_ACT_GELU);
+        a.out[(size_t)(m0 + m) * a.N + n0 + n] = mx4_result<BF16>(y + to_float<BF16>(bias), a.act == W4A4_ACT_GELU);
     }
 }
 
@@ -160,14 +160,14 @@ int launch(A16Args a, hipStream_t st) {
 }
 
 // Fitted to 110 sizes of 1 to 64 tokens, over which the choice is 1 % above the best of the four, 25 % at worst.
-constexpr MX4Way kWays[] = {{16, 16, 2.48f, 0.106f, 0.087f, 0.655f}, {16, 32, 2.65f, 0.155f, 0.128f, 1.403f}, {32, 32, 3.22f, 0.272f, 0.195f, 5.505f}, {32, 64, 3.60f, 0.396f, 0.270f, 0.495f}};
+constexpr MX4Way kWays[] = {{16, 16, 2.48f, 0.106f, 0.087f, 0.655f, 0.0f}, {16, 32, 2.65f, 0.155f, 0.128f, 1.403f, 0.0f}, {32, 32, 3.22f, 0.272f, 0.195f, 5.505f, 0.0f}, {32, 64, 3.60f, 0.396f, 0.270f, 0.495f, 0.0f}};
 
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_a16_kernel<BF16, 1, 1, 8, 2>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
-    switch (mx4_way(kWays, 4, a.M, a.N, mx4_planes(a.K), cus)) {
+    switch (mx4_way(kWays, 4, a.M, a.N, mx4_planes(a.K), a.act, cus)) {
         case 0: return launch<BF16, 1, 1>(a, st);
         case 1: return launch<BF16, 1, 2>(a, st);
         case 2: return launch<BF16, 2, 2>(a, st);

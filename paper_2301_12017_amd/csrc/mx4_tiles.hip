@@ -36,15 +36,17 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
     constexpr int CODES = ROWS / 16, SCALES = ROWS / 64;           // DMA instructions of a plane
     constexpr int CPW = CODES / NW, SPW = (SCALES + NW - 1) / NW, LD = CPW + SPW;               // of a wave
     constexpr int PLANE = ROWS * 68, STAGE = KS * PLANE, NM = FM * FN, NF = FM + FN, RPS = (NF + NM - 2) / (NM - 1);   // operand reads behind a product
-    static_assert(BM % 64 == 0 && BN % 64 == 0 && CODES % NW == 0, "whole DMA instructions, the same number for every wave");
+    static_assert((FN == 2 || FN == 4) && BM % 64 == 0 && BN % 64 == 0 && CODES % NW == 0, "whole DMA instructions, the same number for every wave");
     static_assert((NS - 1) * LD <= 63, "ring depth");
     uint8_t *dummy = smem + NS * STAGE;                            // of waves that have no exponents to fetch
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ks = all / NW, wave = all % NW, wm = wave / WN, wn = wave % WN;
     const int h = lane >> 5, cc = lane & 31;
     const int a_row = wm * FM * 32 + cc, w_row = wn * FN * 32 + cc * FN, n = n0 + w_row;  // of the lane's first fragments, in the tile; its first channel
-    float bias[FN];                                                // (requested in front of the tile's DMA: loads return in order)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) bias[j] = g.bias && n + j < g.N && ks == 0 ? to_float<BF16>(g.bias[n + j]) : 0.0f;
+    // the lane's biases (zeros past the last channel), requested in front of the tile's DMA: loads return in order
+    const __amdgpu_buffer_rsrc_t bias_rsrc = make_rsrc(g.bias, g.bias && ks == 0 ? (uint32_t)g.N * 2 : 0);
+    u32x2 bias = {0, 0};
+    if constexpr (FN == 4) bias = __builtin_amdgcn_raw_buffer_load_b64(bias_rsrc, n * 2, 0, 0);
+    else bias[0] = __builtin_amdgcn_raw_buffer_load_b32(bias_rsrc, n * 2, 0, 0);
 
     // ---- what this wave fetches of a stage ----
     int voff[CPW];
@@ -115,7 +117,7 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = bias[j];
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = to_float<BF16>((uint16_t)(bias[j / 2] >> (16 * (j % 2))));
     u32x4_t P[2][NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f) P[0][f] = read(f, 0, 0);
@@ -186,6 +188,7 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
 #pragma unroll
                     for (int j = 0; j < FN; ++j) y[j] = acc[i][j][e];
                     f((uint32_t)(wm * FM * 32 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) * (uint32_t)g.N * 2 + col, y);
+                    if (e % 2) __builtin_amdgcn_sched_barrier(0);  // (or more of it is begun at once than there are registers for)
                 }
         } else {
             const float *sums = reinterpret_cast<const float *>(smem) + wave * (NM * 16 * 64) + lane;
