@@ -44,18 +44,24 @@ __device__ __forceinline__ uint16_t mx4_result(float y, bool gelu) {
 
 // Tiles of a product.  A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us
 // by tiles of one kind: small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s, whatever is asked for at once), large ones
-// bring less in all.
+// bring less in all.  Past the `held` tiles of a CU the count lies halfway between tiles and whole rounds of them.
 struct MX4Way {
-    int bm, bn;
+    int bm, bn, held;                                              // held: by a CU at once; 0: not counted in rounds
     float start, plane, more, tile, gelu;                          // gelu: more of `tile` where there is one
+    bool tail;                                                     // a last round of up to a quarter is taken in quarters of tiles
 };
 inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int act, int cus) {
     int best = 0;
     float least = INFINITY;
     for (int i = 0; i < count; ++i) {
         const MX4Way &w = ways[i];
-        const float tiles = (float)(((long)M + w.bm - 1) / w.bm) * (float)(((long)N + w.bn - 1) / w.bn), rest = tiles / (float)cus - 1.0f;
-        const float us = w.start + w.plane * (float)planes + (rest > 0.0f ? (w.more * (float)planes + w.tile + (act == W4A4_ACT_GELU ? w.gelu : 0.0f)) * rest : 0.0f);
+        const long tiles = (((long)M + w.bm - 1) / w.bm) * (((long)N + w.bn - 1) / w.bn), left = tiles % cus;
+        float r = (float)tiles / (float)cus;
+        if (w.held && r > (float)w.held) {
+            const long round = (long)w.held * cus, rounds = (tiles + round - 1) / round;
+            r = w.tail && 4 * left <= cus ? (float)(tiles / cus) + (left ? 0.4f : 0.0f) : 0.5f * (r + (float)(rounds * w.held));
+        }
+        const float us = w.start + w.plane * (float)planes + (r > 1.0f ? (w.more * (float)planes + w.tile + (act == W4A4_ACT_GELU ? w.gelu : 0.0f)) * (r - 1.0f) : 0.0f);
         if (us < least) least = us, best = i;
     }
     return best;

@@ -81,12 +81,17 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
     }
 }
 
-// The constants are fitted to 100 to 110 sizes of 1 to 16538 tokens; over 150 sizes the choice is 3 % above the best of fourteen kinds, 27 % at worst.
-constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
+// The constants are fitted to 90 to 178 sizes each, of 1 to 20000 tokens; over 215 sizes the choice is 2.5 % above the best, 28 % at worst.
 // (us of 16384 x 16384 x 1024 without GELU | with it, from 64 x 128 on: 267 | 291, 202 | 235, 194 | 248, 205 | 273.)
-constexpr MX4Way kWays[] = {{16, 16, 2.03f, 0.043f, 0.032f, 0.209f, 0.0f},  {16, 32, 2.13f, 0.056f, 0.061f, 0.464f, 0.0f},    {32, 32, 2.35f, 0.069f, 0.074f, 0.705f, 0.0f},
-                            {64, 64, 4.14f, 0.096f, 0.132f, 2.735f, 0.1f},  {64, 128, 2.97f, 0.247f, 0.178f, 0.839f, 0.19f},  {128, 128, 3.23f, 0.274f, 0.260f, 2.162f, 0.52f},
-                            {128, 256, 4.14f, 0.413f, 0.587f, 3.836f, 1.7f}, {256, 256, 5.53f, 0.583f, 1.327f, 9.544f, 4.5f}};
+constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
+constexpr MX4Way kWays[] = {{16, 16, 0, 1.99f, 0.042f, 0.041f, 0.205f, 0.00f},
+                            {16, 32, 0, 2.10f, 0.056f, 0.061f, 0.551f, 0.00f},
+                            {32, 32, 0, 2.26f, 0.070f, 0.079f, 0.820f, 0.00f},
+                            {64, 64, 1, 4.11f, 0.100f, 0.114f, 3.401f, 0.10f},
+                            {64, 128, 4, 2.75f, 0.267f, 0.134f, 1.075f, 0.19f},
+                            {128, 128, 3, 3.28f, 0.288f, 0.166f, 2.642f, 0.52f},
+                            {128, 256, 2, 4.16f, 0.454f, 0.351f, 4.569f, 1.70f},
+                            {256, 256, 1, 5.85f, 0.625f, 0.765f, 11.804f, 4.50f, true}};
 
 template <bool BF16, int MT, int NT, int NW>
 int launch_few(MX4LinearArgs a, hipStream_t st) {

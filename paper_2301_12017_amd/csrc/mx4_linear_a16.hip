@@ -160,7 +160,7 @@ int launch(A16Args a, hipStream_t st) {
 }
 
 // Fitted to 110 sizes of 1 to 64 tokens, over which the choice is 1 % above the best of the four, 25 % at worst.
-constexpr MX4Way kWays[] = {{16, 16, 2.48f, 0.106f, 0.087f, 0.655f, 0.0f}, {16, 32, 2.65f, 0.155f, 0.128f, 1.403f, 0.0f}, {32, 32, 3.22f, 0.272f, 0.195f, 5.505f, 0.0f}, {32, 64, 3.60f, 0.396f, 0.270f, 0.495f, 0.0f}};
+constexpr MX4Way kWays[] = {{16, 16, 0, 2.48f, 0.106f, 0.087f, 0.655f, 0.0f}, {16, 32, 0, 2.65f, 0.155f, 0.128f, 1.403f, 0.0f}, {32, 32, 0, 3.22f, 0.272f, 0.195f, 5.505f, 0.0f}, {32, 64, 0, 3.60f, 0.396f, 0.270f, 0.495f, 0.0f}};
 
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
