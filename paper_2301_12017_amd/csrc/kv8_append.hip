@@ -386,10 +386,6 @@ __global__ __launch_bounds__(256, POSITIONS == kKeys && D <= 128 ? 3 : 1) void k
         which = __builtin_amdgcn_readfirstlane((blockIdx.y - (values ? quads : 0)) * 4 + wave);
         if (values && which >= a.H) return;
         window = Window{angles, angles + kWindow * a.r.pairs, reinterpret_cast<int *>(angles + 2 * kWindow * a.r.pairs), 0, 0};
-        if (!values) {
-            window.fill(a, blockIdx.x * a.tile, a.tile == 1 ? 1 : kWindow);
-            __syncthreads();
-        }
     } else {
         if (which >= 2 * a.H) return;
         if (values) which -= a.H;
@@ -397,7 +393,12 @@ __global__ __launch_bounds__(256, POSITIONS == kKeys && D <= 128 ? 3 : 1) void k
     const int t_first = blockIdx.x * a.tile, t_last = min(t_first + a.tile, a.T), mask = (1 << a.shift) - 1;
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> a.shift) < a.blocks ? slot >> a.shift : -1; };   // -1: not stored
     // slots of the token before the tile and of the 63 from its first one on; where runs begin; where a slot does not follow the one before
-    const int at = t_first - 1 + lane, slot = at >= 0 && at < a.T ? a.slots[at] : -1, b = block_of(slot);
+    const int at = t_first - 1 + lane, read = a.slots[min(max(at, 0), a.T - 1)];
+    if (ROTARY && !values) {                                       // (while the slots are on their way)
+        window.fill(a, t_first, a.tile == 1 ? 1 : kWindow);
+        __syncthreads();
+    }
+    const int slot = at >= 0 && at < a.T ? read : -1, b = block_of(slot);
     const int b_before = __shfl_up(b, 1, 64), slot_before = __shfl_up(slot, 1, 64);
     const unsigned long long begins = __ballot(lane > 0 && b != b_before), jumps = __ballot(lane > 0 && slot != slot_before + 1);
     const unsigned long long firsts = __ballot(b >= 0 && (slot & mask) == 0);
