@@ -5,6 +5,9 @@ Its layers are the encoder's (post-LayerNorm, GELU feed-forward) with causal att
     x  = LN1(x + attn_out(attention(qkv(x))))        qkv, attn_out, ffn1, ffn2: w4a4_linear_w4a16 (4-bit weights, fp16 activations)
     x  = LN2(x + ffn2(gelu(ffn1(x))))                attention: w4a4_kv8_append, w4a4_kv8_attention
 
+Weights may be in microscaled 4-bit floating point instead (weights="mx4"): few tokens go through w4a4_mx4_linear_a16, more of them, prompts above all, are
+quantized and go through w4a4_mx4_linear.  Positions come from a table of embeddings, or queries and keys are turned by them (angles: w4a4_kv8_append_rotary).
+
 A step takes any number of new tokens of each request (a prompt, a few, one, none, or the end of a request); w4a4_kv8_plan keeps the books of
 blocks on the device.  All layers share one block table.  `python -m paper_2301_12017_amd.decoder` runs random weights.
 """
@@ -35,52 +38,83 @@ class Books:
         return call
 
 
-class DecoderLayer:
-    """One layer: 4-bit weights in groups, a cache of `blocks` blocks.  heads: of queries; kv_heads: of keys and values (grouped heads)."""
+# Tokens up to which microscaled weights meet activations as they are: the weights are read again for every 64 of them.  us of the product with 16-bit
+# activations | of quantizer and product, 4096 x 4096: 32 tokens 7 | 7, 64 10 | 7, 128 20 | 9.
+FEW = 64
 
-    def __init__(self, Wqkv, bqkv, Wo, bo, W1, b1, W2, b2, g1, be1, g2, be2, heads: int, kv_heads: int, blocks: int, block=16, group=128, mode=B.SYM, eps=1e-12):
+
+def quantized(W: torch.Tensor, weights="int4", mode=B.SYM, group=128):
+    """W [N, K] (fp16) in the 4-bit form asked for: integer codes in groups ("int4") or microscaled floating point ("mx4")."""
+    if weights not in ("int4", "mx4"):
+        raise ValueError(f"weights {weights!r}: int4 or mx4")
+    return B.quantize_weight(W, mode, group) if weights == "int4" else B.mx4_quantize(W)
+
+
+def linear(x: torch.Tensor, W, bias=None, act=B.ACT_NONE) -> torch.Tensor:
+    """x [tokens, K] (fp16) times what `quantized` made."""
+    if isinstance(W, B.QWeight):
+        return B.linear_w4a16(x, W, bias, act)
+    if len(x) <= FEW:
+        return B.mx4_linear_a16(x, W, bias, act)
+    return B.mx4_linear(B.mx4_quantize(x), W, bias, act, x.dtype)
+
+
+class DecoderLayer:
+    """One layer: 4-bit weights (see `quantized`), a cache of `blocks` blocks.  heads: of queries; kv_heads: of keys and values (grouped heads).  angles: what
+    queries and keys are turned by (RotaryAngles), None where positions are in the embeddings."""
+
+    def __init__(self, Wqkv, bqkv, Wo, bo, W1, b1, W2, b2, g1, be1, g2, be2, heads: int, kv_heads: int, blocks: int, block=16, group=128, mode=B.SYM, eps=1e-12,
+                 weights="int4", angles=None):
         hidden = Wo.shape[0]
         self.heads, self.kv_heads, self.features, self.eps = heads, kv_heads, Wo.shape[1] // heads, eps
         assert Wqkv.shape == ((heads + 2 * kv_heads) * self.features, hidden)
-        self.qkv, self.out, self.ffn1, self.ffn2 = (B.quantize_weight(W, mode, group) for W in (Wqkv, Wo, W1, W2))
+        self.qkv, self.out, self.ffn1, self.ffn2 = (quantized(W, weights, mode, group) for W in (Wqkv, Wo, W1, W2))
         self.bias = (bqkv, bo, b1, b2)
-        self.ln1, self.ln2 = (g1, be1), (g2, be2)
+        self.ln1, self.ln2, self.angles = (g1, be1), (g2, be2), angles
         self.cache = B.KVCache8.new(blocks, kv_heads, self.features, block, device=Wo.device)
 
     def __call__(self, x: torch.Tensor, books: Books, plan: B.PreparedKV8Plan, queries: int) -> torch.Tensor:
         T, D = x.shape[0], self.features
-        q, k, v = (t.view(T, -1, D) for t in B.linear_w4a16(x, self.qkv, self.bias[0]).split([self.heads * D, self.kv_heads * D, self.kv_heads * D], 1))
-        B.kv8_append(self.cache, k, v, plan.slots)
+        q, k, v = (t.view(T, -1, D) for t in linear(x, self.qkv, self.bias[0]).split([self.heads * D, self.kv_heads * D, self.kv_heads * D], 1))
+        if self.angles is None:
+            B.kv8_append(self.cache, k, v, plan.slots)
+        else:
+            q = B.kv8_append_rotary(self.cache, k, v, plan.slots, plan.positions, self.angles, q)
         a = B.kv8_attention(q, self.cache, books.table, plan.lens, plan.start, queries, books.context, D ** -0.5, workspace=books.workspace)
-        x = self._norm(B.linear_w4a16(a.view(T, -1), self.out, self.bias[1]), x, self.ln1)
-        h = B.linear_w4a16(x, self.ffn1, self.bias[2], B.ACT_GELU)
-        return self._norm(B.linear_w4a16(h, self.ffn2, self.bias[3]), x, self.ln2)
+        x = self._norm(linear(a.view(T, -1), self.out, self.bias[1]), x, self.ln1)
+        h = linear(x, self.ffn1, self.bias[2], B.ACT_GELU)
+        return self._norm(linear(h, self.ffn2, self.bias[3]), x, self.ln2)
 
     def _norm(self, x, residual, ln):
         return B.layernorm_quantize(x, residual, ln[0], ln[1], self.eps)[1]
 
 
 class Decoder:
-    """Token and position embeddings, layers, and the logits of the tokens' successors from the quantized token embeddings."""
+    """Token and position embeddings (positions None: the layers turn queries and keys), layers, and the logits of the tokens' successors from the
+    quantized token embeddings."""
 
-    def __init__(self, layers, tokens: torch.Tensor, positions: torch.Tensor, books: Books, group=128):
-        if len(positions) < books.context:                 # (the plan hands out every position of a block, and they are looked up unseen)
+    def __init__(self, layers, tokens: torch.Tensor, positions, books: Books, group=128, weights="int4"):
+        if positions is None and not all(layer.angles for layer in layers):
+            raise ValueError("no position embeddings, and layers without angles")
+        if positions is not None and len(positions) < books.context:       # (the plan hands out every position of a block, and they are looked up unseen)
             raise ValueError(f"{len(positions)} position embeddings for requests of up to {books.context} tokens")
         self.layers, self.tokens, self.positions, self.books = layers, tokens, positions, books
         pad = -len(tokens) % 8                             # (the linear's channels come in eights)
-        self.head = B.quantize_weight(torch.nn.functional.pad(tokens, (0, 0, 0, pad)).contiguous(), B.SYM, group)
+        self.head = quantized(torch.nn.functional.pad(tokens, (0, 0, 0, pad)).contiguous(), weights, B.SYM, group)
 
     def step(self, ids: torch.Tensor, new_tokens: torch.Tensor, queries: int):
         """ids [tokens]: the new tokens of all requests, one after the other, new_tokens [requests] of them each and `queries` at most.  Returns the
         hidden states [tokens, hidden] and the plan; tokens of requests that found no blocks hold nothing that means anything."""
         plan = self.books.plan(new_tokens, ids.numel())
-        x = self.tokens[ids] + self.positions[plan.positions.clamp(min=0).long()]
+        x = self.tokens[ids]
+        if self.positions is not None:
+            x = x + self.positions[plan.positions.clamp(min=0).long()]
         for layer in self.layers if len(x) else ():        # (a step in which requests only end has no tokens)
             x = layer(x, self.books, plan, queries)
         return x, plan
 
     def logits(self, x: torch.Tensor) -> torch.Tensor:
-        return B.linear_w4a16(x, self.head)[:, :len(self.tokens)]
+        return linear(x, self.head)[:, :len(self.tokens)]
 
     def generate(self, prompts, new: int) -> torch.Tensor:
         """The `new` likeliest next tokens [requests, new], one at a time, behind prompts (a list of 1-D tensors of ids, one or more each).  Requests
@@ -107,28 +141,34 @@ class Decoder:
         return torch.stack(found, 1)
 
 
-def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabulary=1000, requests=4, context=512, block=16, group=128, mode=B.SYM, seed=0) -> Decoder:
-    """Random weights of the given sizes, and blocks for `requests` requests of `context` tokens."""
+def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabulary=1000, requests=4, context=512, block=16, group=128, mode=B.SYM, seed=0,
+                   weights="int4", rotary=False) -> Decoder:
+    """Random weights of the given sizes, and blocks for `requests` requests of `context` tokens.  rotary: no position embeddings, queries and keys turn."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     normal = lambda *shape, std=0.02: (torch.randn(shape, generator=g, device="cuda") * std).half()
     D, blocks = hidden // heads, requests * -(-context // block)
     books = Books(requests, context, blocks, block)
+    angles = B.RotaryAngles(B.rotary_frequencies(D // 2)[0]) if rotary else None
     one = lambda: (1 + normal(hidden, std=0.05).float()).half()
     made = [DecoderLayer(normal((heads + 2 * kv_heads) * D, hidden, std=0.05), normal((heads + 2 * kv_heads) * D), normal(hidden, heads * D), normal(hidden),
                          normal(ffn, hidden), normal(ffn), normal(hidden, ffn), normal(hidden), one(), normal(hidden), one(), normal(hidden),
-                         heads, kv_heads, blocks, block, group, mode) for _ in range(layers)]
-    return Decoder(made, normal(vocabulary, hidden, std=1.0), normal(books.context, hidden, std=0.3), books, group)
+                         heads, kv_heads, blocks, block, group, mode, weights=weights, angles=angles) for _ in range(layers)]
+    return Decoder(made, normal(vocabulary, hidden, std=1.0), None if rotary else normal(books.context, hidden, std=0.3), books, group, weights)
 
 
 if __name__ == "__main__":
     import time
-    decoder = random_decoder(layers=12, ffn=4096, vocabulary=32000, requests=16, context=2048)
     draw = torch.Generator().manual_seed(1)
     prompts = [torch.randint(0, 32000, (100 + 37 * i,), generator=draw) for i in range(16)]
-    decoder.generate(prompts, 2)
-    torch.cuda.synchronize()
-    began = time.perf_counter()
-    found = decoder.generate(prompts, 64)
-    torch.cuda.synchronize()
-    took = time.perf_counter() - began
-    print(f"12 layers of 768, 16 requests of 100 to 655 tokens: {found.numel()} tokens in {took:.3f} s ({found.numel() / took:.0f} a second), prompts included")
+    for kind in ({}, {"weights": "mx4", "rotary": True}):
+        decoder = random_decoder(layers=12, ffn=4096, vocabulary=32000, requests=16, context=2048, **kind)
+        took = []
+        for new in (1, 64):
+            decoder.generate(prompts, new)
+            torch.cuda.synchronize()
+            began = time.perf_counter()
+            found = decoder.generate(prompts, new)
+            torch.cuda.synchronize()
+            took.append(time.perf_counter() - began)
+        print(f"{kind.get('weights', 'int4')}{', rotary' if kind else ''}: 12 layers of 768, 16 requests of 100 to 655 tokens: prompts and their first tokens in "
+              f"{1e3 * took[0]:.1f} ms, {found.numel()} tokens in {took[1]:.3f} s ({found.numel() / took[1]:.0f} a second), prompts included")

@@ -336,6 +336,18 @@ def test_a16(B, M, N, K, gelu, dtype):
     _close(got.cpu(), x @ v.t() + b.double(), x.abs() @ v.abs().t() + b.double().abs(), K + 1, t, gelu)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K", [(264, 1056), (5000, 544), (13000, 288), (16000, 1056)])
+def test_a16_rows_do_not_depend_on_the_others(B, N, K, dtype):
+    """A row's bits are the same whatever rows come with it: every kind of tile adds up in one order."""
+    g, t = _gen(N), TYPES[dtype]
+    X = torch.randn((64, K), generator=g).to(t).cuda()
+    W, b = B.mx4_quantize(torch.randn((N, K), generator=g).to(t).cuda()), torch.randn((N,), generator=g).to(t).cuda()
+    want = B.mx4_linear_a16(X, W, b, B.ACT_GELU)
+    for M in (1, 7, 16, 17, 32, 33, 50):
+        assert torch.equal(B.mx4_linear_a16(X[:M], W, b, B.ACT_GELU), want[:M]), M
+
+
 def test_a16_takes_every_exponent(B):
     """Weights from 2^-128 to 2^127, which no 16-bit type holds beside each other; activations that bring them back."""
     g, M, N = _gen(4), 3, 40

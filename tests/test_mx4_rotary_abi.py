@@ -153,3 +153,14 @@ def test_binding_refuses_what_does_not_fit(b):
     angles = b.RotaryAngles([1.0, 0.5], device="cpu")
     with pytest.raises(AssertionError):
         b.rotary(torch.zeros((1, 1, 8), dtype=torch.float16), torch.zeros(1, dtype=torch.int32), angles)
+
+
+def test_decoder_refuses_what_it_cannot_place_or_name(b):
+    import torch
+    from paper_2301_12017_amd import decoder as dec
+    books = dec.Books(3, 64, 12, 16, device="cpu")
+    layer = type("Layer", (), {"angles": None})()
+    with pytest.raises(ValueError):                               # no table of positions, and nothing that turns
+        dec.Decoder([layer], torch.zeros((8, 64), dtype=torch.float16), None, books)
+    with pytest.raises(ValueError):
+        dec.quantized(torch.zeros((8, 64), dtype=torch.float16), "int3")
