@@ -1014,10 +1014,11 @@ def kv8_attention(q, cache, table, lens, start, queries: int, context: int, scal
 class _PreparedOn(_Prepared):
     """A prepared call that runs on its tensors' device, whatever the current one is: on that device's current stream."""
 
-    def _on(self, *tensors):
-        devices = {t.device for t in tensors if t is not None}
-        assert len(devices) == 1 and next(iter(devices)).type == "cuda", f"tensors on {devices}: one GPU"
-        self.device = next(iter(devices))
+    def _on(self, first, *others):
+        self.device = device = first.device
+        assert first.is_cuda, f"a tensor on {device}: a GPU"
+        for t in others:
+            assert t is None or t.device == device, f"tensors on {device} and {t.device}: one GPU"
 
     def __call__(self, stream=None):
         now = torch.cuda.current_device()
@@ -1056,9 +1057,10 @@ class RotaryAngles:
         turns = [round(Fraction(x) / _TWO_PI * 2 ** 64) % 2 ** 64 for x in f.tolist()]
         self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64).to(device)
         self.pairs, self.interleaved, self.magnitude = f.numel(), bool(interleaved), float(magnitude)
+        self._c = [_RotaryAngles(_address(self.turns), self.pairs, int(self.interleaved), self.magnitude, inverse) for inverse in (0, 1)]
 
     def c(self, inverse=False) -> _RotaryAngles:
-        return _RotaryAngles(_address(self.turns), self.pairs, int(self.interleaved), self.magnitude, int(bool(inverse)))
+        return self._c[bool(inverse)]
 
 
 _TWO_PI = 2 * Fraction("3.14159265358979323846264338327950288419716939937510")
@@ -1131,6 +1133,7 @@ class MX4:
         assert K > 0 and K % 32 == 0 and planes == -(-K // 128) and q.shape == (planes, self.rows, 64), f"{tuple(q.shape)}, {tuple(scale.shape)}: planes of {K} numbers"
         assert q.dtype == torch.uint8 and scale.dtype == torch.int32 and all(t.is_cuda and t.is_contiguous() for t in (q, scale))
         self.q, self.scale = q, scale
+        self._c = _MX4(_address(q), _address(scale), self.rows, K)
 
     @classmethod
     def new(cls, rows: int, K: int, device="cuda"):
@@ -1150,7 +1153,7 @@ class MX4:
         return cls(q, e.view(torch.int32)[..., 0].contiguous(), 2 * half)
 
     def c(self) -> _MX4:
-        return _MX4(_address(self.q), _address(self.scale), self.rows, self.K)
+        return self._c
 
 
 def _rows16(X: torch.Tensor) -> int:
