@@ -662,7 +662,7 @@ typedef struct {
     uint8_t  *q;        /* [ceil(K/128), rows, 64]: q[c][r] holds numbers 128c .. 128c+127 of row r, number 2j in bits 0..3 of byte j
                            and 2j+1 in bits 4..7 (sign, two bits of exponent, one of mantissa); zeros behind K      */
     uint32_t *scale;    /* [ceil(K/128), rows]: byte j of scale[c][r] is 127 + the exponent of row r's block 4c + j; 255: the block is NaN; 0 behind K */
-    int rows, K;        /* K: a multiple of 32                                                                   */
+    int rows, K;        /* K: a multiple of 32, 2^30 at most                                                      */
 } w4a4_mx4;
 
 /* Rows X [out->rows, ldx] (first out->K columns) in `dtype` to out.  A block's exponent is floor(log2(its largest magnitude)) - 2, -127 at least; its numbers

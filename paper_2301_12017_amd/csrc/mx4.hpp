@@ -71,7 +71,7 @@ inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int 
 inline int mx4_check(const w4a4_mx4 *Q) {
     if (!Q || Q->rows < 0 || Q->K <= 0) return W4A4_ERR_INVALID_ARG;
     if (Q->rows && (!Q->q || !Q->scale)) return W4A4_ERR_INVALID_ARG;
-    if (Q->K % 32 || !aligned16(Q->q) || (reinterpret_cast<uintptr_t>(Q->scale) & 3)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    if (Q->K % 32 || Q->K > 1 << 30 || !aligned16(Q->q) || (reinterpret_cast<uintptr_t>(Q->scale) & 3)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     return W4A4_OK;
 }
 

@@ -146,9 +146,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void mx4_linear_a16_kernel(A16Args
     }
 }
 
-template <bool BF16, int MT, int NT>
+template <bool BF16, int MT, int NT, int NW>
 int launch(A16Args a, hipStream_t st) {
-    constexpr int NW = 8;
     auto kern = mx4_linear_a16_kernel<BF16, MT, NT, NW, 2>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
@@ -159,19 +158,23 @@ int launch(A16Args a, hipStream_t st) {
     return launch_status();
 }
 
-// Fitted to 110 sizes of 1 to 64 tokens, over which the choice is 1 % above the best of the four, 25 % at worst.
-constexpr MX4Way kWays[] = {{16, 16, 0, 2.48f, 0.106f, 0.087f, 0.655f, 0.0f}, {16, 32, 0, 2.65f, 0.155f, 0.128f, 1.403f, 0.0f}, {32, 32, 0, 3.22f, 0.272f, 0.195f, 5.505f, 0.0f}, {32, 64, 0, 3.60f, 0.396f, 0.270f, 0.495f, 0.0f}};
+// Tokens and channels of a tile, waves that share K.  Fitted to 200 sizes of 1 to 64 tokens, over which the choice is 2.5 % above the best of eleven kinds, 28 % at
+// worst.  (Few waves where there are many tiles: 64 tokens 32000 x 768 16 us by four waves, 27 by eight; one token 4096 x 4096 5.5 by four, 4.8 by eight.)
+constexpr MX4Way kWays[] = {{16, 16, 0, 2.405f, 0.114f, 0.099f, 0.224f, 0.0f}, {16, 16, 0, 2.596f, 0.087f, 0.103f, 0.448f, 0.0f}, {16, 32, 0, 2.743f, 0.129f, 0.143f, 0.756f, 0.0f},
+                            {16, 64, 0, 3.126f, 0.273f, 0.218f, 0.531f, 0.0f}, {16, 64, 0, 3.301f, 0.206f, 0.229f, 1.126f, 0.0f}, {32, 64, 0, 3.390f, 0.808f, 0.293f, 1.070f, 0.0f}};
 
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_a16_kernel<BF16, 1, 1, 8, 2>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
-    switch (mx4_way(kWays, 4, a.M, a.N, mx4_planes(a.K), a.act, cus)) {
-        case 0: return launch<BF16, 1, 1>(a, st);
-        case 1: return launch<BF16, 1, 2>(a, st);
-        case 2: return launch<BF16, 2, 2>(a, st);
-        default: return launch<BF16, 2, 4>(a, st);
+    switch (mx4_way(kWays, (int)(sizeof(kWays) / sizeof(kWays[0])), a.M, a.N, mx4_planes(a.K), a.act, cus)) {
+        case 0: return launch<BF16, 1, 1, 4>(a, st);
+        case 1: return launch<BF16, 1, 1, 8>(a, st);
+        case 2: return launch<BF16, 1, 2, 8>(a, st);
+        case 3: return launch<BF16, 1, 4, 4>(a, st);
+        case 4: return launch<BF16, 1, 4, 8>(a, st);
+        default: return launch<BF16, 2, 4, 2>(a, st);
     }
 }
 

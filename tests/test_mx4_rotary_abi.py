@@ -23,7 +23,7 @@ def _mx4(b, rows=8, K=64, q=P, scale=P):
 
 def _bad_operands(b):
     return ([(_mx4(b, **kw), -1) for kw in ({"rows": -1}, {"K": 0}, {"K": -32}, {"q": None}, {"scale": None})] +
-            [(_mx4(b, **kw), -2) for kw in ({"K": 48}, {"K": 33}, {"q": P + 8}, {"scale": P + 2})])
+            [(_mx4(b, **kw), -2) for kw in ({"K": 48}, {"K": 33}, {"K": (1 << 30) + 32}, {"q": P + 8}, {"scale": P + 2})])
 
 
 def test_mx4_quantize_and_dequantize_refusals(b):
