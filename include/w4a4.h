@@ -674,7 +674,7 @@ int w4a4_mx4_quantize(const void *X, int dtype, int ldx, const w4a4_mx4 *out, vo
 int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *stream);
 
 /* out[M,N] = act(A * W^T + bias[N]), A [M, K] and W [N, K], bias (may be NULL) and out in `dtype`, fp32 sums, GELU on the fp32 value.
- * N a multiple of 8; out dense, 16-byte aligned as the operands' codes and the bias are. */
+ * N a multiple of 8 (from 2^22 on M * N is 2^33 at most); out dense, 16-byte aligned as the operands' codes and the bias are. */
 int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream);
 
 /* The same with activations X [M, ldx] (first W->K columns) in `dtype`, not quantized: for up to 64 tokens, where the bytes of W are the cost (W is read again for

@@ -1148,8 +1148,9 @@ class MX4:
         rows, half = codes.shape
         assert codes.dtype == exponents.dtype == torch.uint8 and exponents.shape == (rows, half // 16) and half % 16 == 0
         pad = -half % 64
-        q = torch.nn.functional.pad(codes, (0, pad)).view(rows, -1, 64).transpose(0, 1).contiguous()
-        e = torch.nn.functional.pad(exponents, (0, pad // 16)).view(rows, -1, 4).transpose(0, 1).contiguous()
+        planes = (half + pad) // 64
+        q = torch.nn.functional.pad(codes, (0, pad)).reshape(rows, planes, 64).transpose(0, 1).contiguous()
+        e = torch.nn.functional.pad(exponents, (0, pad // 16)).reshape(rows, planes, 4).transpose(0, 1).contiguous()
         return cls(q, e.view(torch.int32)[..., 0].contiguous(), 2 * half)
 
     def c(self) -> _MX4:

@@ -226,6 +226,9 @@ __device__ __forceinline__ unsigned short gelu_erf_half(float x) {
 
 inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
+// Whether a launch of so many workgroups is one: its threads are counted in 32 bits.
+inline bool grid_fits(long groups, int threads) { return groups <= 0xFFFFFFFFL / threads; }
+
 inline int launch_status() {
     return hipGetLastError() == hipSuccess ? W4A4_OK : W4A4_ERR_HIP;
 }

@@ -628,8 +628,10 @@ extern "C" int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_ro
     };
     auto queries = [&](int heads) { return rotary_work(T->q, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, heads); };
     if (T->q && T->tokens <= kFewTokens) return keys(std::integral_constant<Positions, kKeysAndQueries>{}, queries(1));
+    const RotaryWork q = T->q ? queries(4) : RotaryWork{};
+    if (!grid_fits(T->tokens / (T->q && q.share < kPiece ? q.share : kPiece) + 1L, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     if (const int rc = keys(std::integral_constant<Positions, kKeys>{}, RotaryWork{})) return rc;
-    return T->q ? rotary_launch(queries(4), T->dtype, 4, st) : W4A4_OK;
+    return T->q ? rotary_launch(q, T->dtype, 4, st) : W4A4_OK;
 }
 
 extern "C" int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream) {

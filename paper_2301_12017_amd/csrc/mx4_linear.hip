@@ -99,6 +99,7 @@ int launch_few(MX4LinearArgs a, hipStream_t st) {
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
     const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
+    if (!grid_fits(tiles, NW * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
     return launch_status();
 }

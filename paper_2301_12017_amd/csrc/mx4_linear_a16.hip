@@ -152,6 +152,7 @@ int launch(A16Args a, hipStream_t st) {
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
     const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
+    if (!grid_fits(tiles, NW * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     static KernelState ks;
     if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);

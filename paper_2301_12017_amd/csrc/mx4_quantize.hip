@@ -126,7 +126,7 @@ extern "C" int w4a4_mx4_quantize(const void *X, int dtype, int ldx, const w4a4_m
     const bool few = (long)a.rows * cols < 4096;
     const int per = few ? 4 : 16;                                  // rows of a workgroup
     const long groups = ((long)a.rows + per - 1) / per * cols;
-    if (groups > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    if (!grid_fits(groups, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const dim3 grid((unsigned)groups);
     auto run = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, as_stream(stream), a); };
     if (dtype == W4A4_BF16) few ? run(mx4_quantize_kernel<true, 1>) : run(mx4_quantize_kernel<true, 4>);
@@ -140,7 +140,7 @@ extern "C" int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *
     if (Q->rows == 0) return W4A4_OK;
     if (!X) return W4A4_ERR_INVALID_ARG;
     const long groups = ((long)Q->rows + 15) / 16 * ((Q->K + 511) / 512);
-    if (!aligned16(X) || groups > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(X) || !grid_fits(groups, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     const dim3 grid((unsigned)groups);
     auto run = [&](auto kern) {
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, as_stream(stream), Q->q, Q->scale, Q->rows, Q->K, static_cast<uint16_t *>(X));

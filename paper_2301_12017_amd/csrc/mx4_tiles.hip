@@ -266,6 +266,7 @@ int launch(MX4LinearArgs g, hipStream_t st) {
     g.tiles_m = (int)(((long)g.M + BM - 1) / BM);
     g.tiles_n = (int)(((long)g.N + BN - 1) / BN);
     const long tiles = (long)g.tiles_m * g.tiles_n;
+    if (!grid_fits(tiles, WM * WN * KS * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks);
     if (cus < 0) return W4A4_ERR_HIP;

@@ -50,5 +50,7 @@ extern "C" int w4a4_rotary(const void *X, int dtype, int tokens, int heads, int 
     if (!aligned16(X) || !aligned16(out)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     // Four heads of a thread share its angles, where there are tokens enough for all CUs.
     const int at_once = (long)tokens * heads * features < 256L * 256 * 8 * 4 ? 1 : 4;
-    return rotary_launch(rotary_work(X, tokens, heads, features, ldx, positions, rotary_args(R), out, ldo, at_once), dtype, at_once, as_stream(stream));
+    const RotaryWork work = rotary_work(X, tokens, heads, features, ldx, positions, rotary_args(R), out, ldo, at_once);
+    if (!grid_fits(((long)tokens + work.share - 1) / work.share, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    return rotary_launch(work, dtype, at_once, as_stream(stream));
 }

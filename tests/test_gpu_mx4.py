@@ -160,6 +160,14 @@ def test_operands_as_checkpoints_hold_them(B):
     assert got.K == 160 and torch.equal(got.q, want.q) and torch.equal(got.scale, want.scale)
 
 
+def test_operands_as_checkpoints_hold_them_strided_and_none(B):
+    codes, exponents = torch.randint(0, 256, (6, 192), generator=_gen(1)).to(torch.uint8).cuda(), torch.randint(0, 255, (6, 12), generator=_gen(2)).to(torch.uint8).cuda()
+    want, got = B.MX4.from_rows(codes[::2, :128].contiguous(), exponents[::2, :8].contiguous()), B.MX4.from_rows(codes[::2, :128], exponents[::2, :8])
+    assert torch.equal(got.q, want.q) and torch.equal(got.scale, want.scale)
+    none = B.MX4.from_rows(codes[:0], exponents[:0])
+    assert (none.rows, none.K) == (0, 384) and B.mx4_linear(none, B.MX4.from_rows(codes.repeat(4, 1), exponents.repeat(4, 1))).shape == (0, 24)
+
+
 # ---- products ----------------------------------------------------------------------------------------------------------------
 def _exact_operand(g, rows, K):
     """Numbers that are multiples of 1/2 up to 24 (exponents 0 .. 2)."""

@@ -43,6 +43,8 @@ def test_mx4_quantize_and_dequantize_refusals(b):
     assert quantize(_mx4(b, rows=0), X=None) == 0 and dequantize(_mx4(b, rows=0, q=None, scale=None), X=None) == 0
     large = _mx4(b, rows=BIG, K=32768)                            # more workgroups than a grid has
     assert quantize(large, ldx=32768) == -2 and dequantize(large) == -2
+    many = _mx4(b, rows=(1 << 28) + 1, K=64)                      # a thread more than a launch counts
+    assert quantize(many) == -2 and dequantize(many) == -2
 
 
 def test_mx4_linear_refusals(b):
@@ -97,6 +99,7 @@ def test_rotary_refusals(b):
     assert f(X=None) == -1 and f(out=None) == -1 and f(positions=None) == -1 and f(out=P, ldo=136) == -1
     assert f(features=68, ldx=136, ldo=136) == -2 and f(features=264, ldx=528, ldo=528) == -2 and f(ldx=132) == -2 and f(ldo=130) == -2 and f(X=P + 2) == -2 and f(out=P + 8) == -2
     assert f(heads=BIG, features=256) == -1
+    assert f(tokens=(1 << 28) + 1, heads=16, features=128, ldx=2048, ldo=2048, R=_angles(b, interleaved=1)) == -2      # more threads than a launch counts
     assert f(tokens=0, X=None, out=None, positions=None) == 0
 
 
@@ -122,6 +125,7 @@ def test_kv8_append_rotary_refusals(b):
     for kw in ({"ldk": 132}, {"ldv": 132}, {"k": P + 8}, {"v": P + 2}, {"ldq": 260}, {"q": P + 8}, {"q_out": P + 4}):
         assert f(**kw) == -2, kw
     assert f(tokens=0) == 0 and f(tokens=0, k=None, positions=None) == 0
+    assert f(tokens=1 << 28) == -2 and f(tokens=BIG, q=None, q_out=None) == -2       # more threads than a launch counts
 
 
 def test_calls_laid_out_once_reach_their_entry_point(b):
