@@ -20,9 +20,10 @@
 namespace w4a4 {
 namespace {
 
-enum Positions { kNone, kKeys, kKeysAndQueries };                   // what turns on the way
+enum Positions { kNone, kKeys, kKeysAndQueries };                  // what turns on the way
 
 constexpr int kPiece = 16;                                         // tokens of a run that a wave takes at once
+constexpr int kQueryHeads = 4;                                     // of a thread, which share its angles
 
 struct AppendArgs {
     int8_t *k, *v;
@@ -31,6 +32,7 @@ struct AppendArgs {
     long ld[2];
     const int32_t *slots;
     int T, blocks, H, shift, tile;
+    int waves, window, query_tile;                                 // that share a run; tokens whose angles are there at once; tokens whose queries a workgroup turns
     const int32_t *positions;                                      // keys that turn
     RotaryArgs r;
     RotaryWork q;                                                  // the step's queries
@@ -70,15 +72,15 @@ __device__ __forceinline__ uint32_t finite2(uint32_t w) {          // what does 
 }
 
 // The scale of a unit (a head's block) that had the scale `had` after tokens of range `wide`; what stays of the block is re-scaled where it
-// rises.  Returns the scale's reciprocal.
-__device__ __forceinline__ float settle(float *scale, float had, int8_t *codes, int bytes, bool first, float wide, int lane) {
+// rises, by `waves` waves of which this is one.  Returns the scale's reciprocal.
+__device__ __forceinline__ float settle(float *scale, float had, int8_t *codes, int bytes, bool first, float wide, int lane, int part = 0, int waves = 1) {
     const float was = first ? 0.0f : had;
     float now = fmaxf(was, wide / 127.0f);
     if (now < 1.1754943508e-38f) now = 0.0f;                       // (its reciprocal would not be a number)
     if (!first && now != was) {
         const float ratio = now > 0.0f ? was / now : 0.0f;
 #pragma unroll 4
-        for (int i = 16 * lane; i < bytes; i += 16 * 64) {
+        for (int i = 16 * (lane + 64 * part); i < bytes; i += 16 * 64 * waves) {
             u32x4_t p = *reinterpret_cast<const u32x4_t *>(codes + i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -91,74 +93,21 @@ __device__ __forceinline__ float settle(float *scale, float had, int8_t *codes, 
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // the new codes, other lanes', come behind these
     }
-    if (lane == 0 && now != had) *scale = now;
+    if (lane == 0 && part == 0 && now != had) *scale = now;
     return now > 0.0f ? 1.0f / now : 0.0f;
 }
 
-// The features d .. d+7 of a key (a lane's, in w), turned: `other` holds their partners where pairs are halves, cosines and sines of the token's pairs lie in LDS.
-template <bool BF16>
-__device__ __forceinline__ void turn8(const RotaryArgs &r, u32x4_t w, u32x4_t other, int d, const float *cosines, const float *sines, float (&to)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) to[j] = to_float<BF16>((uint16_t)(w[j / 2] >> (16 * (j % 2))));
-    if (r.interleaved) {
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            const int p = (d + j) / 2;
-            if (p >= r.pairs) break;
-            const Turn t{cosines[p], sines[p]};
-            const float u = to[j], v = to[j + 1];
-            to[j] = turned_a(t, u, v);
-            to[j + 1] = turned_b(t, u, v);
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int f = d + j, p = f < r.pairs ? f : f - r.pairs;
-        if (f >= 2 * r.pairs) break;
-        const Turn t{cosines[p], sines[p]};
-        const float v = to_float<BF16>((uint16_t)(other[j / 2] >> (16 * (j % 2))));
-        to[j] = f < r.pairs ? turned_a(t, to[j], v) : turned_b(t, v, to[j]);
-    }
-}
-
-// Cosines and sines of the pairs of kWindow tokens from `first` on, and those tokens' positions, in LDS: found by all four waves of a workgroup together.
-constexpr int kWindow = 32;
-struct Window {
-    float *cosines, *sines;                                        // [kWindow][pairs]
-    int *positions;                                                // [kWindow]
-    int first, count;
-    __device__ __forceinline__ void fill(const AppendArgs &a, int from, int tokens) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.r.pairs;
-        first = from;
-        count = min(tokens, a.T - from);
-        if ((int)threadIdx.x < count) positions[threadIdx.x] = a.positions[from + threadIdx.x];
-        for (int p = lane; p < pairs; p += 64) {
-            const uint64_t per = a.r.turns[p];
-            for (int t = wave; t < count; t += 4) {
-                const Turn turn = turn_of(per, (uint32_t)a.positions[from + t], a.r.magnitude, a.r.inverse);
-                cosines[t * pairs + p] = turn.cos;
-                sines[t * pairs + p] = turn.sin;
-            }
-        }
-    }
-};
-
 // Keys: tokens t0 .. t1-1 into the block's rows.
-// ROTARY: the four waves of a workgroup have four heads (h past the last one: nothing) and do the same steps, and find the angles together.
-template <bool BF16, int D, bool ROTARY>
-__device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane, Window &window) {
+template <bool BF16, int D>
+__device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane) {
     constexpr int LANES = D / 8, ROWS = 64 / LANES, N = (kPiece + ROWS - 1) / ROWS;   // lanes of a row, rows at once, loads of a chunk
     const int block = 1 << a.shift, row = lane / LANES;
-    const bool there = !ROTARY || h < a.H;
-    const bool on = row < ROWS && there;
-    if (!there) h = 0;
+    const bool on = row < ROWS;
     const uint16_t *x = a.x[0] + h * D + lane % LANES * 8;
     const size_t unit = (size_t)b * a.H + h;
     int8_t *codes = a.k + unit * D * block;
     const float had = a.k_scale[unit];
     u32x4_t w[N];
-    float turned[ROTARY ? N : 1][8];
     auto load = [&](int c) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -167,113 +116,250 @@ __device__ __forceinline__ void append_keys(const AppendArgs &a, int t0, int t1,
             if (on && t < t1) w[i] = *reinterpret_cast<const u32x4_t *>(x + t * a.ld[0]);
         }
     };
-    auto load_turned = [&](int c) {
-        const int pairs = a.r.pairs, d = lane % LANES * 8;
-        u32x4_t other[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {                              // (rows that are not there: the last one again)
-            const uint16_t *p = x + min(c + i * ROWS + min(row, ROWS - 1), t1 - 1) * a.ld[0];
-            w[i] = *reinterpret_cast<const u32x4_t *>(p);
-            if (a.r.interleaved || d >= 2 * pairs) continue;
-            if (pairs % 8 == 0) {
-                other[i] = *reinterpret_cast<const u32x4_t *>(d < pairs ? p + pairs : p - pairs);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t o[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int f = d + 2 * j + e;
-                        o[e] = p[f < pairs ? 2 * j + e + pairs : f < 2 * pairs ? 2 * j + e - pairs : 2 * j + e];
-                    }
-                    other[i][j] = o[0] | o[1] << 16;
-                }
-            }
-        }
-        if (c < window.first || min(c + N * ROWS, t1) > window.first + window.count) {
-            __syncthreads();                                       // (the angles before have been read)
-            window.fill(a, c, kWindow);
-            __syncthreads();
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int t = c + i * ROWS + min(row, ROWS - 1), at = min(t, t1 - 1) - window.first;
-            if (window.positions[at] >= 0) {
-                turn8<BF16>(a.r, w[i], other[i], d, window.cosines + at * pairs, window.sines + at * pairs, turned[ROTARY ? i : 0]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) turned[ROTARY ? i : 0][j] = to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2))));
-            }
-            if (!on || t >= t1)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) turned[ROTARY ? i : 0][j] = 0.0f;
-        }
-    };
-    auto range = [&](bool careful) {                               // (of turned keys the bits of an fp32 number)
+    auto range = [&](bool careful) {
         Range m;
-        uint32_t most = 0;
         for (int c = t0; c < t1; c += N * ROWS) {
-            if constexpr (ROTARY) load_turned(c);
-            else load(c);
+            load(c);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (ROTARY) {
+            for (int i = 0; i < N; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t bits = __builtin_bit_cast(uint32_t, turned[i][j]) & 0x7FFFFFFFu;
-                        most = max(most, careful && bits >= 0x7F800000u ? 0u : bits);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) m.take(careful ? finite2<BF16>(w[i][j]) : w[i][j]);
-                }
-            }
+                for (int j = 0; j < 4; ++j) m.take(careful ? finite2<BF16>(w[i][j]) : w[i][j]);
         }
-        if constexpr (ROTARY) return lanes_reduce<64>(most, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-        else return m.over_wave();
+        return m.over_wave();
     };
     uint32_t wide = range(false);
-    bool careful = wide >= (ROTARY ? 0x7F800000u : kInf<BF16>);
-    if (ROTARY ? __syncthreads_or(careful) : careful) {            // (all waves take the same steps)
-        const uint32_t finite = range(true);
-        if (careful) wide = finite;
-    }
-    float inv = 0.0f;
-    if (there) inv = settle(a.k_scale + unit, had, codes, D * block, first, ROTARY ? __builtin_bit_cast(float, wide) : to_float<BF16>((uint16_t)wide), lane);
+    const bool careful = wide >= kInf<BF16>;
+    if (careful) wide = range(true);
+    const float inv = settle(a.k_scale + unit, had, codes, D * block, first, to_float<BF16>((uint16_t)wide), lane);
     auto write = [&](auto careful) {
         constexpr bool C = decltype(careful)::value;
         for (int c = t0; c < t1; c += N * ROWS) {
-            if (t1 - t0 > N * ROWS) {
-                if constexpr (ROTARY) load_turned(c);
-                else load(c);
-            }
+            if (t1 - t0 > N * ROWS) load(c);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int t = c + i * ROWS + row;
                 if (!on || t >= t1) continue;
                 uint32_t o[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = code8<C>(ROTARY ? turned[ROTARY ? i : 0][j] : to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2)))), inv);
+                for (int j = 0; j < 8; ++j) o[j] = code8<C>(to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2)))), inv);
                 *reinterpret_cast<u32x2_t *>(codes + (size_t)(a.slots[t] & (block - 1)) * D + lane % LANES * 8) =
                     u32x2_t{bytes4(o[0], o[1], o[2], o[3]), bytes4(o[4], o[5], o[6], o[7])};
             }
         }
     };
-    if (ROTARY ? __syncthreads_or(careful) : careful) write(std::true_type{});
+    if (careful) write(std::true_type{});
     else write(std::false_type{});
 }
 
-// Values: tokens t0 .. t1-1 into the block's columns.  ordered: their slots follow each other, from slot `off` of the block on.
+// Where an append has positions, `waves` (1, 2 or 4) of a workgroup's four share a run, chunk by chunk, and so a block of many tokens does not wait for one of them.
+// All four take the same steps.
+struct Share {
+    int waves, part;                                               // this wave's part
+    uint32_t *ranges;                                              // [2][4] in LDS
+    // Largest `mine` of the waves that share; any: one of the workgroup's is `from` or more.
+    __device__ __forceinline__ uint32_t most(uint32_t mine, int use, uint32_t from, bool &any) const {
+        const int wave = threadIdx.x >> 6, first = wave & -waves;
+        if ((threadIdx.x & 63) == 0) ranges[4 * use + wave] = mine;
+        __syncthreads();
+        any = false;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = ranges[4 * use + i];
+            any |= x >= from;                                      // (the same in every wave)
+            if (i >= first && i < first + waves) mine = max(mine, x);
+        }
+        any = __builtin_amdgcn_readfirstlane(any);
+        return __builtin_amdgcn_readfirstlane(mine);
+    }
+};
+
+// Cosines and sines of the pairs of some tokens, and those tokens' positions, in LDS: found by all four waves of a workgroup together.
+struct Window {
+    float *cosines, *sines;                                        // [tokens][pairs]
+    int *positions;
+    uint64_t turns[2];                                             // of the lane's pairs
+    int first, count;
+    __device__ __forceinline__ void open(const AppendArgs &a, float *lds) {
+        const int lane = threadIdx.x & 63, last = a.r.pairs - 1;
+        cosines = lds;
+        sines = lds + a.window * a.r.pairs;
+        positions = reinterpret_cast<int *>(sines + a.window * a.r.pairs);
+        first = count = 0;
+        turns[0] = a.r.turns[min(lane, last)];
+        turns[1] = a.r.turns[min(lane + 64, last)];
+    }
+    __device__ __forceinline__ void fill(const AppendArgs &a, int from, int tokens) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pairs = a.r.pairs;
+        first = from;
+        count = min(tokens, a.T - from);                           // at most 64
+        const int mine = a.positions[from + min(lane, count - 1)];
+        if (count > 1) __syncthreads();                            // (the angles before have been read)
+        if (wave == 0 && lane < count) positions[lane] = mine;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int p = lane + 64 * i;
+            if (p >= pairs) break;
+#pragma unroll 1
+            for (int t = wave; t < count; t += 4) {
+                const Turn turn = turn_of(turns[i], (uint32_t)__builtin_amdgcn_readlane(mine, t), a.r.magnitude, a.r.inverse);
+                cosines[t * pairs + p] = turn.cos;
+                sines[t * pairs + p] = turn.sin;
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// The features d .. d+7 of a key (a lane's, in `to`), turned: cosines and sines of the token's pairs lie in LDS.  `other` holds their partners where pairs are
+// halves and a multiple of eight; of other numbers of pairs they are fetched one by one (x: the lane's features).
+template <bool BF16>
+__device__ __forceinline__ void turn8(const RotaryArgs &r, u32x4_t other, const uint16_t *x, int d, const float *cosines, const float *sines, float (&to)[8]) {
+    if (d >= 2 * r.pairs) return;
+    if (r.pairs % 8 == 0) {                                        // angles four at a time
+        const int p0 = r.interleaved ? d / 2 : d < r.pairs ? d : d - r.pairs;
+        const float4_t *c = reinterpret_cast<const float4_t *>(cosines + p0), *s = reinterpret_cast<const float4_t *>(sines + p0);
+        if (r.interleaved) {
+            const float4_t cs = c[0], sn = s[0];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Turn t{cs[j], sn[j]};
+                const float u = to[2 * j], v = to[2 * j + 1];
+                to[2 * j] = turned_a(t, u, v);
+                to[2 * j + 1] = turned_b(t, u, v);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const Turn t{c[j / 4][j % 4], s[j / 4][j % 4]};
+                const float v = to_float<BF16>((uint16_t)(other[j / 2] >> (16 * (j % 2))));
+                to[j] = d < r.pairs ? turned_a(t, to[j], v) : turned_b(t, v, to[j]);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int f = d + j, p = r.interleaved ? f / 2 : f < r.pairs ? f : f - r.pairs;
+        if (f >= 2 * r.pairs) break;
+        const Turn t{cosines[p], sines[p]};
+        if (r.interleaved) {
+            if (j % 2) continue;
+            const float u = to[j], v = to[j + 1];
+            to[j] = turned_a(t, u, v);
+            to[j + 1] = turned_b(t, u, v);
+        } else {
+            const float v = to_float<BF16>(x[f < r.pairs ? j + r.pairs : j - r.pairs]);
+            to[j] = f < r.pairs ? turned_a(t, to[j], v) : turned_b(t, v, to[j]);
+        }
+    }
+}
+
+// Tokens of a run that a wave turns at once, and waves that may share one (us at 2 | 4: 30000 tokens of 2 heads of 64 in blocks of 128 32 | 43, 12003 of 8 of 128 in
+// blocks of 64 49 | 64; 4000 of 2 heads of 256, whose chunks are shorter, in blocks of 64 37 | 28).
+template <int D>
+struct Turning {
+    static constexpr int LANES = D / 8, ROWS = 64 / LANES, N = D == 64 ? 2 : 4, CHUNK = N * ROWS;    // lanes of a row, rows at once, loads of a chunk
+    static constexpr int WAVES = D == 256 ? 4 : 2;
+};
+
+// Keys with positions: tokens t0 .. t1-1 into the block's rows (h past the last head: nothing, but in step).
 template <bool BF16, int D>
-__device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t1, int b, int h, bool first, bool ordered, int off, int lane) {
+__device__ __forceinline__ void append_turned_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane, Window &window, const Share &share) {
+    constexpr int LANES = Turning<D>::LANES, ROWS = Turning<D>::ROWS, N = Turning<D>::N, CHUNK = Turning<D>::CHUNK;
+    const int block = 1 << a.shift, row = min(lane / LANES, ROWS - 1), d = lane % LANES * 8, pairs = a.r.pairs, step = share.waves * CHUNK;
+    const bool there = h < a.H, on = lane / LANES < ROWS && there;
+    if (!there) h = 0;
+    const uint16_t *x = a.x[0] + h * D + d;
+    const size_t unit = (size_t)b * a.H + h;
+    int8_t *codes = a.k + unit * D * block;
+    float had = a.k_scale[unit], turned[N][8], inv = 0.0f;
+    int slots[N];
+    auto load = [&](int s) {                                       // the wave's chunk of the step from token s on (rows that are not there: the last one again)
+        const int c = s + share.part * CHUNK + row;
+        auto at = [&](int i) { return x + min(c + i * ROWS, t1 - 1) * a.ld[0]; };
+        u32x4_t w[N], other[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w[i] = *reinterpret_cast<const u32x4_t *>(at(i));
+            slots[i] = a.slots[min(c + i * ROWS, t1 - 1)];
+        }
+        if (!a.r.interleaved && pairs % 8 == 0) {
+            const int to = d < pairs ? pairs : d < 2 * pairs ? -pairs : 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) other[i] = *reinterpret_cast<const u32x4_t *>(at(i) + to);
+        }
+        if (s < window.first || min(s + step, t1) > window.first + window.count) window.fill(a, s, a.window);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int t = c + i * ROWS, from = min(t, t1 - 1) - window.first;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) turned[i][j] = to_float<BF16>((uint16_t)(w[i][j / 2] >> (16 * (j % 2))));
+            if (window.positions[from] >= 0) turn8<BF16>(a.r, other[i], at(i), d, window.cosines + from * pairs, window.sines + from * pairs, turned[i]);
+            if (!on || t >= t1)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) turned[i][j] = 0.0f;
+            __builtin_amdgcn_sched_barrier(0);                     // (angles of more rows are more registers than there are)
+        }
+    };
+    // the run's range, that of its finite numbers where there are others (the bits of fp32 numbers), its codes
+    enum { kRange, kFinite, kWrite } pass = kRange;
+    bool careful = false, none;
+    uint32_t most = 0;
+    for (;;) {
+        for (int s = t0; s < t1; s += step) {
+            if (pass == kRange || t1 - t0 > step) load(s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (pass != kWrite) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t bits = __builtin_bit_cast(uint32_t, turned[i][j]) & 0x7FFFFFFFu;
+                        most = max(most, pass == kFinite && bits >= 0x7F800000u ? 0u : bits);
+                    }
+                } else if (on && s + share.part * CHUNK + i * ROWS + row < t1) {
+                    uint32_t o[8];
+                    if (careful) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = code8<true>(turned[i][j], inv);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = code8<false>(turned[i][j], inv);
+                    }
+                    *reinterpret_cast<u32x2_t *>(codes + (size_t)(slots[i] & (block - 1)) * D + d) = u32x2_t{bytes4(o[0], o[1], o[2], o[3]), bytes4(o[4], o[5], o[6], o[7])};
+                }
+            }
+        }
+        if (pass == kWrite) break;
+        most = lanes_reduce<64>(most, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        asm volatile("" : "+v"(had));                              // (has been read before another wave writes it)
+        if (pass == kRange) {
+            most = share.most(most, 0, 0x7F800000u, careful);
+            if (careful) {
+                pass = kFinite;
+                most = 0;
+                continue;
+            }
+        } else {
+            most = share.most(most, 1, ~0u, none);
+        }
+        if (there) inv = settle(a.k_scale + unit, had, codes, D * block, first, __builtin_bit_cast(float, most), lane, share.part, share.waves);
+        __syncthreads();                                           // (the block's old codes are re-scaled)
+        pass = kWrite;
+    }
+}
+
+// Values: tokens t0 .. t1-1 into the block's columns.  ordered: their slots follow each other, from slot `off` of the block on.  SHARED: by the waves that
+// share a run (h past the last head: nothing, but in step).
+template <bool BF16, int D, bool SHARED>
+__device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t1, int b, int h, bool first, bool ordered, int off, int lane, const Share &share) {
     constexpr int F = D == 64 ? 1 : 2, N = D == 256 ? 2 : 1;       // neighbouring features a lane, and times that
     constexpr int FEW = 4;                                         // tokens below which codes are stored byte by byte
     const int block = 1 << a.shift;
-    const bool on = lane * F < D;
+    const bool there = !SHARED || h < a.H, on = lane * F < D && there;
+    if (!there) h = 0;
     const uint16_t *x = a.x[1] + h * D + (on ? lane * F : 0);      // (lanes without a feature: the first one again)
     const size_t unit = (size_t)b * a.H + h;
     int8_t *codes = a.v + unit * D * block;
-    const float had = a.v_scale[unit];
+    float had = a.v_scale[unit];
     uint32_t w[N][kPiece];
     auto load = [&](int t, int i) {                                // the lane's features of token t
 #pragma unroll
@@ -281,7 +367,7 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     };
     // pieces of sixteen slots of the block where the tokens are in order: the first token's place in its piece comes first
     const bool few = t1 - t0 < FEW;
-    const int c0 = ordered && !few ? t0 - (off & (kPiece - 1)) : t0;
+    const int c0 = ordered && !few ? t0 - (off & (kPiece - 1)) : t0, mine = SHARED ? c0 + kPiece * share.part : c0, step = SHARED ? kPiece * share.waves : kPiece;
     auto chunk = [&](int c) {                                      // tokens c .. c + 15; the run's first and last one again where it has none
         if (few) {
 #pragma unroll
@@ -293,8 +379,8 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     };
     auto range = [&](bool careful) {
         Range m;
-        for (int c = c0; c < t1; c += kPiece) {
-            chunk(c);
+        for (int c = mine; c < t1; c += step) {
+            if (!careful || t1 - c0 > step) chunk(c);
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
                 if (i >= FEW - 1 && few) break;
@@ -305,13 +391,23 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
         return m.over_wave();
     };
     uint32_t wide = range(false);
-    const bool careful = wide >= kInf<BF16>;
-    if (careful) wide = range(true);
-    const float inv = settle(a.v_scale + unit, had, codes, D * block, first, to_float<BF16>((uint16_t)wide), lane);
+    bool careful = wide >= kInf<BF16>, none;
+    if constexpr (SHARED) {
+        asm volatile("" : "+v"(had));                              // (has been read before another wave writes it)
+        wide = share.most(wide, 0, kInf<BF16>, careful);
+    }
+    if (careful) {
+        wide = range(true);
+        if constexpr (SHARED) wide = share.most(wide, 1, ~0u, none);
+    }
+    float inv = 0.0f;
+    if (there) inv = settle(a.v_scale + unit, had, codes, D * block, first, to_float<BF16>((uint16_t)wide), lane, SHARED ? share.part : 0, SHARED ? share.waves : 1);
+    if constexpr (SHARED) __syncthreads();                         // (the block's old codes are re-scaled)
     auto write = [&](auto careful) {
         constexpr bool C = decltype(careful)::value;
         auto code = [&](int n, int f, int i) { return code8<C>(to_float<BF16>((uint16_t)(w[n][i] >> (16 * f))), inv); };
         if (few) {
+            if (SHARED && share.part) return;
 #pragma unroll
             for (int i = 0; i < FEW - 1; ++i)
                 if (t0 + i < t1) {
@@ -324,8 +420,8 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
                 }
             return;
         }
-        for (int c = c0; c < t1; c += kPiece) {
-            if (t1 - c0 > kPiece) chunk(c);
+        for (int c = mine; c < t1; c += step) {
+            if (t1 - c0 > step) chunk(c);
             const int lo = max(t0 - c, 0), hi = min(t1 - c, kPiece);                     // tokens lo .. hi-1 of the chunk
             const int at = ordered ? off + (c - t0) : 0;           // (a multiple of 16) slot of the chunk's first token
 #pragma unroll
@@ -362,42 +458,44 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     else write(std::false_type{});
 }
 
-// (Turning keys takes registers that the values' waves would rather do without: with three waves a SIMD asked for, 10002 tokens of 8 heads of 128 take 33 us, with
-// two 39, with four, which spill, 58; without positions 20.)
 template <bool BF16, int D, Positions POSITIONS>
-__global__ __launch_bounds__(256, POSITIONS == kKeys && D <= 128 ? 3 : 1) void kv8_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256, POSITIONS == kNone ? 1 : 3) void kv8_append_kernel(AppendArgs a) {
     constexpr bool ROTARY = POSITIONS != kNone;
-    extern __shared__ float angles[];                              // ROTARY: a window's
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quads = (a.H + 3) / 4;
-    // 0 .. H-1: keys of a head, H .. 2H-1: values.  ROTARY: workgroups of four heads' keys, then of four heads' values, then of queries
-    int which = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);
-    bool values = which >= a.H;
-    Window window{};
-    if constexpr (ROTARY) {
-        if (POSITIONS == kKeysAndQueries && (int)blockIdx.y == 2 * quads) {
+    extern __shared__ __attribute__((aligned(16))) float angles[]; // ROTARY: a window's
+    __shared__ uint32_t ranges[8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int which, tile = blockIdx.x;                                  // 0 .. H-1: keys of a head, H .. 2H-1: values
+    bool values;
+    Window window;
+    Share share{1, 0, ranges};
+    if constexpr (ROTARY) {                                        // workgroups of some heads' keys, all tiles of them, then of values, then of queries
+        const int tiles = (a.T + a.tile - 1) / a.tile, heads = 4 / a.waves, groups = (a.H + heads - 1) / heads, group = blockIdx.x / tiles;
+        if (POSITIONS == kKeysAndQueries && group >= 2 * groups) {
+            const int t0 = ((int)blockIdx.x - 2 * groups * tiles) * a.query_tile, count = min(a.query_tile, a.T - t0);
             switch (a.q.way) {
-                case kRotaryNeighbours: return rotary_tokens<BF16, kRotaryNeighbours, 1>(a.q, blockIdx.x, 1);
-                case kRotaryHalves8: return rotary_tokens<BF16, kRotaryHalves8, 1>(a.q, blockIdx.x, 1);
-                case kRotaryHalves4: return rotary_tokens<BF16, kRotaryHalves4, 1>(a.q, blockIdx.x, 1);
-                default: return rotary_tokens<BF16, kRotarySingle, 1>(a.q, blockIdx.x, 1);
+                case kRotaryNeighbours: return rotary_tokens<BF16, kRotaryNeighbours, kQueryHeads>(a.q, t0, count);
+                case kRotaryHalves8: return rotary_tokens<BF16, kRotaryHalves8, kQueryHeads>(a.q, t0, count);
+                case kRotaryHalves4: return rotary_tokens<BF16, kRotaryHalves4, kQueryHeads>(a.q, t0, count);
+                default: return rotary_tokens<BF16, kRotarySingle, kQueryHeads>(a.q, t0, count);
             }
         }
-        values = (int)blockIdx.y >= quads;
-        which = __builtin_amdgcn_readfirstlane((blockIdx.y - (values ? quads : 0)) * 4 + wave);
-        if (values && which >= a.H) return;
-        window = Window{angles, angles + kWindow * a.r.pairs, reinterpret_cast<int *>(angles + 2 * kWindow * a.r.pairs), 0, 0};
+        tile -= group * tiles;
+        values = group >= groups;
+        which = (group - (values ? groups : 0)) * heads + wave / a.waves;
+        share.waves = a.waves;
+        share.part = wave & (a.waves - 1);
+        if (!values) window.open(a, angles);
     } else {
+        which = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);
         if (which >= 2 * a.H) return;
+        values = which >= a.H;
         if (values) which -= a.H;
     }
-    const int t_first = blockIdx.x * a.tile, t_last = min(t_first + a.tile, a.T), mask = (1 << a.shift) - 1;
+    const int t_first = tile * a.tile, t_last = min(t_first + a.tile, a.T), mask = (1 << a.shift) - 1;
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> a.shift) < a.blocks ? slot >> a.shift : -1; };   // -1: not stored
     // slots of the token before the tile and of the 63 from its first one on; where runs begin; where a slot does not follow the one before
     const int at = t_first - 1 + lane, read = a.slots[min(max(at, 0), a.T - 1)];
-    if (ROTARY && !values) {                                       // (while the slots are on their way)
-        window.fill(a, t_first, a.tile == 1 ? 1 : kWindow);
-        __syncthreads();
-    }
+    if (ROTARY && !values && a.tile == 1) window.fill(a, t_first, 1);                   // (while the slots are on their way)
     const int slot = at >= 0 && at < a.T ? read : -1, b = block_of(slot);
     const int b_before = __shfl_up(b, 1, 64), slot_before = __shfl_up(slot, 1, 64);
     const unsigned long long begins = __ballot(lane > 0 && b != b_before), jumps = __ballot(lane > 0 && slot != slot_before + 1);
@@ -428,8 +526,9 @@ __global__ __launch_bounds__(256, POSITIONS == kKeys && D <= 128 ? 3 : 1) void k
             }
         }
         const int off = __builtin_amdgcn_readlane(slot, i) & mask;
-        if (!values) append_keys<BF16, D, ROTARY>(a, t0, t1, bi, which, first, lane, window);
-        else append_values<BF16, D>(a, t0, t1, bi, which, first, ordered, off, lane);
+        if (values) append_values<BF16, D, ROTARY>(a, t0, t1, bi, which, first, ordered, off, lane, share);
+        else if constexpr (ROTARY) append_turned_keys<BF16, D>(a, t0, t1, bi, which, first, lane, window, share);
+        else append_keys<BF16, D>(a, t0, t1, bi, which, first, lane);
     }
 }
 
@@ -584,20 +683,32 @@ int rows_check(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype,
     return W4A4_OK;
 }
 
-// Up to this many tokens a workgroup has one of them, and the queries turn in the same launch.  (Behind it, where memory is what counts, queries have a launch
-// of their own: their registers would leave the keys half as many waves.)
-constexpr int kFewTokens = 512;
-
 template <Positions POSITIONS>
 int append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv, const int32_t *slots, const int32_t *positions,
            const RotaryArgs &r, const RotaryWork &q, hipStream_t st) {
     AppendArgs a{C->k, C->v, C->k_scale, C->v_scale, {static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V)}, {ldk, ldv},
-                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= kFewTokens ? 1 : kPiece, positions, r, q};
-    const dim3 grid((tokens + a.tile - 1) / a.tile, POSITIONS == kNone ? (2 * C->heads + 3) / 4 : 2 * ((C->heads + 3) / 4) + (POSITIONS == kKeysAndQueries));
+                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece, 1, 0, 1, positions, r, q};
     return by_features(C->features, [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        static_assert((kPiece + 64 / (D / 8) - 1) / (64 / (D / 8)) * (64 / (D / 8)) <= kWindow, "a chunk of rows has its angles in one window");
-        const size_t lds = POSITIONS != kNone ? (size_t)kWindow * (2 * r.pairs + 1) * sizeof(float) : 0;          // at most 33 KB
+        constexpr int D = decltype(d)::value, CHUNK = Turning<D>::CHUNK, WAVES = Turning<D>::WAVES;
+        static_assert(WAVES * CHUNK <= 64, "a lane each");
+        size_t lds = 0;
+        dim3 grid((tokens + a.tile - 1) / a.tile, (2 * C->heads + 3) / 4);
+        if (POSITIONS != kNone) {
+            const int share = C->block / (D == 256 ? 8 : 16);
+            a.waves = share < WAVES ? share : WAVES;
+            // (a workgroup for a token each: sharing leaves few of its waves something to do, so not where there are many; 200 tokens of 8 heads of 64 13 us shared, 8 not)
+            if (a.tile == 1 && (long)tokens * C->heads * a.waves > 2048) a.waves = 1;
+            a.window = a.waves * CHUNK;
+            lds = (size_t)a.window * (2 * r.pairs + 1) * sizeof(float);                 // at most 33 KB
+            // Tokens of a workgroup: where there are thousands, prompts are among them, and most workgroups of sixteen would meet no first token of a block (us at
+            // 16 | at most 63: 30000 tokens of 2 heads of 64 in blocks of 128 77 | 43, 2000 of 8 of 128 in blocks of 32 19 | 15; but 600 single tokens of 8 heads 65 | 213).
+            const int heads = 4 / a.waves, groups = (C->heads + heads - 1) / heads;
+            if (tokens >= 4096) a.tile = C->block < 63 ? C->block : 63;
+            a.query_tile = tokens <= 512 ? 1 : 16;
+            const long tiles = (tokens + (long)a.tile - 1) / a.tile, all = tiles * 2 * groups + (POSITIONS == kKeysAndQueries ? (tokens + (long)a.query_tile - 1) / a.query_tile : 0);
+            if (!grid_fits(all, 256)) return (int)W4A4_ERR_UNSUPPORTED_SHAPE;
+            grid = dim3((unsigned)all);
+        }
         if (dtype == W4A4_BF16) hipLaunchKernelGGL((kv8_append_kernel<true, D, POSITIONS>), grid, dim3(256), lds, st, a);
         else hipLaunchKernelGGL((kv8_append_kernel<false, D, POSITIONS>), grid, dim3(256), lds, st, a);
         return launch_status();
@@ -626,12 +737,9 @@ extern "C" int w4a4_kv8_append_rotary(const w4a4_kv8_cache *C, const w4a4_kv8_ro
     auto keys = [&](auto positions, const RotaryWork &q) {
         return append<decltype(positions)::value>(C, T->k, T->v, T->dtype, T->tokens, T->ldk, T->ldv, T->slots, T->positions, r, q, st);
     };
-    auto queries = [&](int heads) { return rotary_work(T->q, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, heads); };
-    if (T->q && T->tokens <= kFewTokens) return keys(std::integral_constant<Positions, kKeysAndQueries>{}, queries(1));
-    const RotaryWork q = T->q ? queries(4) : RotaryWork{};
-    if (!grid_fits(T->tokens / (T->q && q.share < kPiece ? q.share : kPiece) + 1L, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    if (const int rc = keys(std::integral_constant<Positions, kKeys>{}, RotaryWork{})) return rc;
-    return T->q ? rotary_launch(q, T->dtype, 4, st) : W4A4_OK;
+    if (!T->q) return keys(std::integral_constant<Positions, kKeys>{}, RotaryWork{});
+    return keys(std::integral_constant<Positions, kKeysAndQueries>{},
+                rotary_work(T->q, T->tokens, T->heads, C->features, T->ldq, T->positions, r, T->q_out, (long)T->heads * C->features, kQueryHeads));
 }
 
 extern "C" int w4a4_kv8_read(const w4a4_kv8_cache *C, const int32_t *slots, int tokens, int dtype, void *K, void *V, void *stream) {

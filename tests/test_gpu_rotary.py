@@ -304,6 +304,36 @@ def test_append_rotary_on_both_sides_of_its_tiles(B, T, tile):
     assert _same(one, many) and torch.equal(got, B.rotary(q, positions, angles))
 
 
+@pytest.mark.parametrize("T", [700, 4500])
+@pytest.mark.parametrize("D,block,H", [(64, 128, 3), (96, 64, 3), (128, 32, 5), (256, 16, 3), (256, 128, 1)])
+def test_append_rotary_of_runs_that_waves_share(B, D, block, H, T):
+    """A prompt in two parts that meet inside a block, whose scale the second one raises: rows that do not turn are stored as w4a4_kv8_append stores them, numbers
+    that are not finite among them, and rows that turn as a call for each block stores them."""
+    g, t = _gen(D + block), torch.float16
+    blocks, half = -(-T // block) + 1, T // 2 + 3
+    order = torch.randperm(blocks, generator=g)
+    at = torch.arange(T) + 5
+    slots = (order[at // block] * block + at % block).int()
+    k, v = ((torch.randn((T, H, D), generator=g) * torch.where(torch.arange(T) < half, 1, 8)[:, None, None]).to(t) for _ in range(2))
+    still, C = torch.full((T,), -1, dtype=torch.int32).cuda(), _cache(B, g, blocks, H, D, block)
+    plain, angles, parts = _clone(B, C), _angles(B, D // 2, False), ((0, half), (half, T))
+    odd_k, odd_v = k.clone(), v.clone()
+    odd_k[3, 0, 1], odd_k[half + 40, H - 1, D - 1], odd_v[17, H - 1, 2], odd_v[T - 1, 0, 0] = float("nan"), float("inf"), -float("inf"), float("nan")
+    for lo, hi in parts:
+        B.kv8_append(plain, odd_k[lo:hi].cuda(), odd_v[lo:hi].cuda(), slots[lo:hi].cuda())
+        B.kv8_append_rotary(C, odd_k[lo:hi].cuda(), odd_v[lo:hi].cuda(), slots[lo:hi].cuda(), still[lo:hi], angles)
+        assert _same(C, plain)
+    positions = (torch.arange(T, dtype=torch.int32) + 1000).cuda()
+    C = _cache(B, _gen(1), blocks, H, D, block)
+    by_block = _clone(B, C)
+    for lo, hi in parts:
+        B.kv8_append_rotary(C, k[lo:hi].cuda(), v[lo:hi].cuda(), slots[lo:hi].cuda(), positions[lo:hi], angles)
+        edges = [lo] + [i for i in range(lo + 1, hi) if (i + 5) % block == 0] + [hi]
+        for a, b in zip(edges, edges[1:]):
+            B.kv8_append_rotary(by_block, k[a:b].cuda(), v[a:b].cuda(), slots[a:b].cuda(), positions[a:b], angles)
+    assert _same(C, by_block)
+
+
 def test_captured_and_replayed(B):
     g, H, G, D, block, T = _gen(9), 2, 6, 64, 16, 30
     angles = _angles(B, 32, True)
