@@ -159,10 +159,12 @@ int launch(A16Args a, hipStream_t st) {
     return launch_status();
 }
 
-// Tokens and channels of a tile, waves that share K.  Fitted to 200 sizes of 1 to 64 tokens, over which the choice is 2.5 % above the best of eleven kinds, 28 % at
-// worst.  (Few waves where there are many tiles: 64 tokens 32000 x 768 16 us by four waves, 27 by eight; one token 4096 x 4096 5.5 by four, 4.8 by eight.)
+// Tokens and channels of a tile, waves that share K.  Fitted to 200 sizes of 1 to 64 tokens each; over 200 with weights that no cache holds the choice is 2.2 % above the
+// best of nine kinds, 32 % at worst.  us of the kinds in their order: one token 4096 x 4096 5.5, 4.8, ..; 32 tokens 16000 x 4096 (23 by the third), 20, 19, 32, 17; 64 tokens
+// 32000 x 768 (28), 17, 22, 16, 22.
 constexpr MX4Way kWays[] = {{16, 16, 0, 2.405f, 0.114f, 0.099f, 0.224f, 0.0f}, {16, 16, 0, 2.596f, 0.087f, 0.103f, 0.448f, 0.0f}, {16, 32, 0, 2.743f, 0.129f, 0.143f, 0.756f, 0.0f},
-                            {16, 64, 0, 3.126f, 0.273f, 0.218f, 0.531f, 0.0f}, {16, 64, 0, 3.301f, 0.206f, 0.229f, 1.126f, 0.0f}, {32, 64, 0, 3.390f, 0.808f, 0.293f, 1.070f, 0.0f}};
+                            {16, 64, 0, 3.126f, 0.273f, 0.218f, 0.531f, 0.0f}, {16, 64, 0, 3.301f, 0.206f, 0.229f, 1.126f, 0.0f}, {32, 64, 0, 3.390f, 0.808f, 0.293f, 1.070f, 0.0f},
+                            {32, 64, 0, 3.698f, 0.296f, 1.413f, 0.000f, 0.0f}};
 
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
@@ -175,7 +177,8 @@ int pick(const A16Args &a, hipStream_t st) {
         case 2: return launch<BF16, 1, 2, 8>(a, st);
         case 3: return launch<BF16, 1, 4, 4>(a, st);
         case 4: return launch<BF16, 1, 4, 8>(a, st);
-        default: return launch<BF16, 2, 4, 2>(a, st);
+        case 5: return launch<BF16, 2, 4, 2>(a, st);
+        default: return launch<BF16, 2, 4, 8>(a, st);
     }
 }
 
