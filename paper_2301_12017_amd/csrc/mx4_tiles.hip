@@ -213,23 +213,19 @@ __device__ __forceinline__ void tile(const MX4LinearArgs &g, uint8_t *smem, int 
         });
         return;
     }
-    float finite = 0.0f;                                           // NaN where a sum is none or infinite: those are done again, with care
     results([&](uint32_t at, float (&y)[FN]) {
+        float finite = 0.0f;                                       // NaN where a sum is none or infinite: those are done again, with care
 #pragma unroll
         for (int j = 0; j < FN; j += 2) {
             finite = __fmaf_rn(y[j], 0.0f, __fmaf_rn(y[j + 1], 0.0f, finite));
             w[j / 2] = mx4_gelu2<BF16>(y[j], y[j + 1]);
         }
-        store_words<FN / 2, kStreamed>(out, at, w);
-    });
-    if (finite == 0.0f) return;
-    results([&](uint32_t at, float (&y)[FN]) {
+        if (__builtin_expect(finite != 0.0f, 0))
 #pragma unroll
-        for (int j = 0; j < FN; j += 2) {
-            w[j / 2] = mx4_gelu2<BF16>(y[j], y[j + 1]);
-            if (!(fabsf(y[j]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFF0000u) | from_float<BF16>(mx4_gelu_limit(y[j]));
-            if (!(fabsf(y[j + 1]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFFu) | (uint32_t)from_float<BF16>(mx4_gelu_limit(y[j + 1])) << 16;
-        }
+            for (int j = 0; j < FN; j += 2) {
+                if (!(fabsf(y[j]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFF0000u) | from_float<BF16>(mx4_gelu_limit(y[j]));
+                if (!(fabsf(y[j + 1]) < INFINITY)) w[j / 2] = (w[j / 2] & 0xFFFFu) | (uint32_t)from_float<BF16>(mx4_gelu_limit(y[j + 1])) << 16;
+            }
         store_words<FN / 2, kStreamed>(out, at, w);
     });
 }
