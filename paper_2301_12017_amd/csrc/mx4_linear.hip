@@ -81,17 +81,17 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
     }
 }
 
-// The constants are fitted to 90 to 178 sizes each, of 1 to 20000 tokens; over 215 sizes the choice is 2.5 % above the best, 28 % at worst.
-// (us of 16384 x 16384 x 1024 without GELU | with it, from 64 x 128 on: 267 | 291, 202 | 235, 194 | 248, 205 | 273.)
+// The constants are fitted to 90 to 178 sizes each, of 1 to 20000 tokens; over 215 sizes the choice is 2.4 % above the best, 28 % at worst.
+// (us of 16384 x 16384 x 1024 without GELU | with it, from 64 x 128 on: 254 | 292, 202 | 241, 195 | 229, 205 | 264.)
 constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
 constexpr MX4Way kWays[] = {{16, 16, 0, 1.99f, 0.042f, 0.041f, 0.205f, 0.00f},
                             {16, 32, 0, 2.10f, 0.056f, 0.061f, 0.551f, 0.00f},
                             {32, 32, 0, 2.26f, 0.070f, 0.079f, 0.820f, 0.00f},
                             {64, 64, 1, 4.11f, 0.100f, 0.114f, 3.401f, 0.10f},
-                            {64, 128, 4, 2.75f, 0.267f, 0.134f, 1.075f, 0.19f},
-                            {128, 128, 3, 3.28f, 0.288f, 0.166f, 2.642f, 0.52f},
-                            {128, 256, 2, 4.16f, 0.454f, 0.351f, 4.569f, 1.70f},
-                            {256, 256, 1, 5.85f, 0.625f, 0.765f, 11.804f, 4.50f, true}};
+                            {64, 128, 4, 2.75f, 0.267f, 0.147f, 0.932f, 0.28f},
+                            {128, 128, 3, 3.28f, 0.288f, 0.198f, 2.149f, 0.60f},
+                            {128, 256, 2, 4.16f, 0.454f, 0.399f, 3.798f, 1.40f},
+                            {256, 256, 1, 5.85f, 0.625f, 0.851f, 9.643f, 3.50f, true}};
 
 template <bool BF16, int MT, int NT, int NW>
 int launch_few(MX4LinearArgs a, hipStream_t st) {
