@@ -4,6 +4,9 @@
 //
 // The matrix instruction takes codes and exponents as they are: 128 numbers of 16 rows, a lane one block of one row, sixteen bytes of codes
 // and a byte of exponent.  A plane's rows follow each other, so such an operand is a kilobyte of consecutive memory.
+//
+// This file's kernel takes what has too few tiles for the one in LDS (mx4_tiles.hip): a chain of first loads, a product, a sum over eight waves.  5 tokens
+// 1024 x 1024 2.7 us, of which a launch is 2.1.
 #include "mx4.hpp"
 #include "mx4_linear.hpp"
 

@@ -3,6 +3,9 @@
 //   a' = m (a cos(p f) - b sin(p f)),  b' = m (b cos(p f) + a sin(p f))    for each pair (a, b) of features, p the position, f the pair's frequency
 //
 // Features behind the turned part are copied.
+//
+// Memory bounds it: 8191 tokens of 32 heads of 128, 26.4 us = 5.1 TB/s read and written, what a copy of them takes (halves of a head as pairs: 28).
+// Few tokens are a launch and the latency of their loads: 16 of 12 heads of 64 3.1 us.
 #include "rotary.hpp"
 
 namespace w4a4 {
@@ -48,7 +51,8 @@ extern "C" int w4a4_rotary(const void *X, int dtype, int tokens, int heads, int 
     if (!X || !out || !positions) return W4A4_ERR_INVALID_ARG;
     if (X == out && ldx != ldo) return W4A4_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(out)) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    // Four heads of a thread share its angles, where there are tokens enough for all CUs.
+    // Four heads of a thread share its angles, where there are tokens enough for all CUs.  us by one | four: 16 tokens of 12 heads of 64 3.1 | 3.5, 400 of 32 of 128 4.2 | 4.3,
+    // 600 5.0 | 4.5, 8191 33 | 28.
     const int at_once = (long)tokens * heads * features < 256L * 256 * 8 * 4 ? 1 : 4;
     const RotaryWork work = rotary_work(X, tokens, heads, features, ldx, positions, rotary_args(R), out, ldo, at_once);
     if (!grid_fits(((long)tokens + work.share - 1) / work.share, 256)) return W4A4_ERR_UNSUPPORTED_SHAPE;
