@@ -192,10 +192,10 @@ struct Window {
     }
     __device__ __forceinline__ void fill(const AppendArgs &a, int from, int tokens) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pairs = a.r.pairs;
+        if (count) __syncthreads();                                // (the angles before have been read)
         first = from;
         count = min(tokens, a.T - from);                           // at most 64
         const int mine = a.positions[from + min(lane, count - 1)];
-        if (count > 1) __syncthreads();                            // (the angles before have been read)
         if (wave == 0 && lane < count) positions[lane] = mine;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

@@ -334,6 +334,27 @@ def test_append_rotary_of_runs_that_waves_share(B, D, block, H, T):
     assert _same(C, by_block)
 
 
+def test_append_rotary_of_a_last_token_behind_a_long_run(B):
+    """A workgroup goes on from a run of several steps to one whose window of angles is the last token alone."""
+    g, H, D, block = _gen(11), 4, 64, 64
+    sizes = [64] * 65 + [6, 41, 1]                                # tokens of each block: those from 66 * 63 on are one workgroup's
+    T = sum(sizes)
+    assert T >= 4096 and T - 42 >= 66 * 63 and T <= 67 * 63
+    slots = torch.cat([b * block + torch.arange(n) for b, n in enumerate(sizes)]).int()
+    positions = torch.randint(0, 5000, (T,), generator=g).int().cuda()
+    k, v = (torch.randn((T, H, D), generator=g).half().cuda() for _ in range(2))
+    angles = _angles(B, 32, False)
+    once, by_block = (B.KVCache8.new(len(sizes), H, D, block) for _ in range(2))
+    B.kv8_append_rotary(once, k, v, slots.cuda(), positions, angles)
+    a = 0
+    for n in sizes:
+        B.kv8_append_rotary(by_block, k[a:a + n], v[a:a + n], slots[a:a + n].cuda(), positions[a:a + n], angles)
+        a += n
+    for b, n in enumerate(sizes):                                 # (what lies behind a block's tokens means nothing)
+        assert torch.equal(once.k[b, :, :n], by_block.k[b, :, :n]) and torch.equal(once.v[b, :, :, :n], by_block.v[b, :, :, :n])
+    assert torch.equal(once.k_scale, by_block.k_scale) and torch.equal(once.v_scale, by_block.v_scale)
+
+
 def test_captured_and_replayed(B):
     g, H, G, D, block, T = _gen(9), 2, 6, 64, 16, 30
     angles = _angles(B, 32, True)
