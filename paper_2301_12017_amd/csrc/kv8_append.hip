@@ -704,9 +704,11 @@ int append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int
             if (a.tile == 1 && (long)tokens * C->heads * a.waves > 2048) a.waves = 1;
             a.window = a.waves * CHUNK;
             lds = (size_t)a.window * (2 * r.pairs + 1) * sizeof(float);                 // at most 33 KB
-            // Tokens of a workgroup: where there are thousands, prompts are among them, and most workgroups of sixteen would meet no first token of a block (us at
-            // 16 | at most 63: 30000 tokens of 2 heads of 64 in blocks of 128 77 | 43, 2000 of 8 of 128 in blocks of 32 19 | 15; but 600 single tokens of 8 heads 65 | 213).
-            const int heads = 4 / a.waves, groups = (C->heads + heads - 1) / heads;
+            // Tokens of a workgroup, whose runs it takes one after the other.  Where there are thousands, prompts are among them, and most workgroups of sixteen would meet
+            // no first token of a block (us at 16 | at most 63: 30000 tokens of 2 heads of 64 in blocks of 128 77 | 32); some hundreds may be requests of one token each (us
+            // at 16 | this: 600 of those, 8 heads of 128 in blocks of 16 61 | 21, 1000 of 64 43 | 36; prompts of 600 and 1000 tokens 10.8 | 13.3 and 13.5 | 15.6).
+            const int heads = 4 / a.waves, groups = (C->heads + heads - 1) / heads, few = tokens / 128;
+            if (tokens > 512 && few < kPiece) a.tile = few;
             if (tokens >= 4096) a.tile = C->block < 63 ? C->block : 63;
             a.query_tile = tokens <= 512 ? 1 : 16;
             const long tiles = (tokens + (long)a.tile - 1) / a.tile, all = tiles * 2 * groups + (POSITIONS == kKeysAndQueries ? (tokens + (long)a.query_tile - 1) / a.query_tile : 0);
