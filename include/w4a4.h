@@ -673,7 +673,8 @@ int w4a4_mx4_quantize(const void *X, int dtype, int ldx, const w4a4_mx4 *out, vo
 /* The numbers that Q stands for, X [rows, K] in `dtype` (bf16 holds them exactly from 2^-126 on; fp16 rounds, and what passes it is an infinity). */
 int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *stream);
 
-/* out[M,N] = act(A * W^T + bias[N]), A [M, K] and W [N, K], bias (may be NULL) and out in `dtype`, fp32 sums, GELU on the fp32 value.
+/* out[M,N] = act(A * W^T + bias[N]), A [M, K] and W [N, K], bias (may be NULL) and out in `dtype`, fp32 sums, GELU on the fp32 value (9e-5 of it before
+ * it is rounded; fp16: of what is no subnormal number, and 1e-8; bf16: of what is 2^-122 or more).
  * N a multiple of 8 (from 2^22 on M * N is 2^33 at most); out dense, 16-byte aligned as the operands' codes and the bias are. */
 int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream);
 
