@@ -26,7 +26,7 @@ __device__ __forceinline__ float mx4_scale(uint32_t e) {
 // log2 Phi(-t) is a polynomial of degree 9 in t, fitted evenly to [0, 13.35] (3.3e-5, or 2.3e-5 of Phi).  Its fp32 steps add 5.0e-5 at most (half a step of each
 // partial sum, at the t behind it), measured 4.3e-5 of GELU in all: 8e-5, a 24th of the smallest half step of bf16, wherever |GELU| is 2^-122 or more.  Below that Phi leaves fp32's normal
 // numbers, and the result may be 0.  Behind 13.3 the polynomial falls on, and x's own size times 2^-inf is 0: x needs no clamp.  (fp16's form, degree 5, is off by 0.3 % at -5 and
-14 % at -7; the four steps more take 16384 x 16384 x 1024 from 226 to 239 us, 12288 x 4096 x 1024 from 54 to 57.)
+// 14 % at -7; the four steps more take 16384 x 16384 x 1024 from 226 to 239 us, 12288 x 4096 x 1024 from 54 to 57.)
 __device__ __forceinline__ float mx4_gelu_bf16(float x) {
     const float t = fabsf(x);
     float q = -1.858528553e-09f;
