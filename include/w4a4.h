@@ -675,11 +675,13 @@ int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *stream);
 
 /* out[M,N] = act(A * W^T + bias[N]), A [M, K] and W [N, K], bias (may be NULL) and out in `dtype`, fp32 sums, GELU on the fp32 value (9e-5 of it before
  * it is rounded; fp16: of what is no subnormal number, and 1e-8; bf16: of what is 2^-122 or more).
- * N a multiple of 8 (from 2^22 on M * N is 2^33 at most); out dense, 16-byte aligned as the operands' codes and the bias are. */
+ * N a multiple of 8; out dense, 16-byte aligned as the operands' codes and the bias are.  A launch is 2^32 threads: ceil(M / 256) * ceil(N / 256) below 2^23
+ * where N is below 2^22, else ceil(M / 32) * ceil(N / 32) below 2^23. */
 int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream);
 
 /* The same with activations X [M, ldx] (first W->K columns) in `dtype`, not quantized: for up to 64 tokens, where the bytes of W are the cost (W is read again for
- * every 64).  A block's 32 products are summed before its power of two comes to them: an |x| past 2^120 may pass fp32 there.  ldx a multiple of 8, below 2^24. */
+ * every 64).  A block's 32 products are summed before its power of two comes to them: an |x| past 2^120 may pass fp32 there.  ldx a multiple of 8, below 2^24;
+ * ceil(M / 32) * ceil(N / 64) below 2^25. */
 int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, const w4a4_mx4 *W, const void *bias, int act, void *out, void *stream);
 
 /* A call of one of the entry points with its arguments laid out once, for callers to whom passing a dozen of them costs as

@@ -61,17 +61,26 @@ __device__ __forceinline__ uint16_t mx4_result(float y, bool gelu) {
 // Tiles of a product.  A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us
 // by tiles of one kind: small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s, whatever is asked for at once), large ones
 // bring less in all.  Past the `held` tiles of a CU the count lies halfway between tiles and whole rounds of them.
+// A kind whose workgroups are more than a launch takes is none.
 struct MX4Way {
-    int bm, bn, held;                                              // held: by a CU at once; 0: not counted in rounds
+    int bm, bn, threads, held;                                     // threads: of a workgroup; held: by a CU at once; 0: not counted in rounds
     float start, plane, more, tile, gelu;                          // gelu: more of `tile` where there is one
     bool tail;                                                     // a last round of up to a quarter is taken in quarters of tiles
 };
+inline long mx4_way_tiles(const MX4Way &w, int M, int N) { return (((long)M + w.bm - 1) / w.bm) * (((long)N + w.bn - 1) / w.bn); }
+inline bool mx4_launches(const MX4Way &w, int M, int N) { return grid_fits(mx4_way_tiles(w, M, N), w.threads); }
+inline bool mx4_any_launches(const MX4Way *ways, int count, int M, int N) {
+    for (int i = 0; i < count; ++i)
+        if (mx4_launches(ways[i], M, N)) return true;
+    return false;
+}
 inline int mx4_way(const MX4Way *ways, int count, int M, int N, int planes, int act, int cus) {
-    int best = 0;
+    int best = -1;
     float least = INFINITY;
     for (int i = 0; i < count; ++i) {
         const MX4Way &w = ways[i];
-        const long tiles = (((long)M + w.bm - 1) / w.bm) * (((long)N + w.bn - 1) / w.bn), left = tiles % cus;
+        if (!mx4_launches(w, M, N)) continue;
+        const long tiles = mx4_way_tiles(w, M, N), left = tiles % cus;
         float r = (float)tiles / (float)cus;
         if (w.held && r > (float)w.held) {
             const long round = (long)w.held * cus, rounds = (tiles + round - 1) / round;

@@ -87,33 +87,34 @@ __global__ __launch_bounds__(NW * 64) void mx4_linear_few_kernel(MX4LinearArgs a
 // The constants are fitted to 90 to 178 sizes each, of 1 to 20000 tokens; over 215 sizes the choice is 2.4 % above the best, 28 % at worst.
 // (us of 16384 x 16384 x 1024 without GELU | with it, from 64 x 128 on: 254 | 292, 202 | 241, 195 | 229, 205 | 264.)
 constexpr int kFew = 3;                                            // the first of them are this file's, the others an MX4Tile each
-constexpr MX4Way kWays[] = {{16, 16, 0, 1.99f, 0.042f, 0.041f, 0.205f, 0.00f},
-                            {16, 32, 0, 2.10f, 0.056f, 0.061f, 0.551f, 0.00f},
-                            {32, 32, 0, 2.26f, 0.070f, 0.079f, 0.820f, 0.00f},
-                            {64, 64, 1, 4.11f, 0.100f, 0.114f, 3.401f, 0.10f},
-                            {64, 128, 4, 2.75f, 0.267f, 0.147f, 0.932f, 0.28f},
-                            {128, 128, 3, 3.28f, 0.288f, 0.198f, 2.149f, 0.60f},
-                            {128, 256, 2, 4.16f, 0.454f, 0.399f, 3.798f, 1.40f},
-                            {256, 256, 1, 5.85f, 0.625f, 0.851f, 9.643f, 3.50f, true}};
+constexpr MX4Way kWays[] = {{16, 16, 512, 0, 1.99f, 0.042f, 0.041f, 0.205f, 0.00f},
+                            {16, 32, 512, 0, 2.10f, 0.056f, 0.061f, 0.551f, 0.00f},
+                            {32, 32, 512, 0, 2.26f, 0.070f, 0.079f, 0.820f, 0.00f},
+                            {64, 64, 512, 1, 4.11f, 0.100f, 0.114f, 3.401f, 0.10f},
+                            {64, 128, 256, 4, 2.75f, 0.267f, 0.147f, 0.932f, 0.28f},
+                            {128, 128, 256, 3, 3.28f, 0.288f, 0.198f, 2.149f, 0.60f},
+                            {128, 256, 256, 2, 4.16f, 0.454f, 0.399f, 3.798f, 1.40f},
+                            {256, 256, 512, 1, 5.85f, 0.625f, 0.851f, 9.643f, 3.50f, true}};
 
 template <bool BF16, int MT, int NT, int NW>
 int launch_few(MX4LinearArgs a, hipStream_t st) {
     auto kern = mx4_linear_few_kernel<BF16, MT, NT, NW>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
-    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
-    if (!grid_fits(tiles, NW * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));     // (mx4_way has asked whether they are a launch)
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
     return launch_status();
 }
 
 template <bool BF16>
 int pick(const MX4LinearArgs &a, hipStream_t st) {
+    // (the tiles in LDS have 32-bit offsets into a row of tiles' results)
+    const int ways = a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew;
+    if (!mx4_any_launches(kWays, ways, a.M, a.N)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_few_kernel<BF16, 1, 1, 8>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
-    // (the tiles in LDS have 32-bit offsets into a row of tiles' results)
-    const int way = mx4_way(kWays, a.N < 1 << 22 ? (int)(sizeof(kWays) / sizeof(kWays[0])) : kFew, a.M, a.N, a.planes, a.act, cus);
+    const int way = mx4_way(kWays, ways, a.M, a.N, a.planes, a.act, cus);
     switch (way) {
         case 0: return launch_few<BF16, 1, 1, 8>(a, st);
         case 1: return launch_few<BF16, 1, 2, 8>(a, st);
@@ -134,7 +135,6 @@ extern "C" int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void 
     if (A->rows == 0) return W4A4_OK;
     if (!out) return W4A4_ERR_INVALID_ARG;
     if (W->rows % 8 || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    if (((long)A->rows / 16 + 1) * ((long)W->rows / 16 + 1) > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;    // (of the smallest tiles: a grid)
     const MX4LinearArgs a{A->q, W->q, A->scale, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), A->rows, W->rows, mx4_planes(A->K), act, 0, 0, 0};
     return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
 }

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void mx4_linear_a16_kernel(A16Args
     const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x + (size_t)m0 * a.ldx, (uint32_t)(((long)min(16 * MT, a.M - m0) - 1) * a.ldx + a.K) * 2);
     const int rows = min(16 * MT, a.M - m0), cols = min(16 * NT, a.N - n0);
     const int n = threadIdx.x % (16 * NT);                         // the channel of the results that the thread finishes
-    const uint16_t bias = __builtin_amdgcn_raw_buffer_load_b16(make_rsrc(a.bias, a.bias ? (uint32_t)a.N * 2 : 0), (n0 + n) * 2, 0, 0);
+    const uint16_t bias = __builtin_amdgcn_raw_buffer_load_b16(make_rsrc(a.bias, a.bias ? (uint32_t)a.N * 2 : 0), (int)((uint32_t)(n0 + n) * 2), 0, 0);
     int xo[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) xo[t] = 16 * t + col < rows ? ((16 * t + col) * a.ldx + 8 * kg) * 2 : (int)kPoison;
@@ -151,8 +151,7 @@ int launch(A16Args a, hipStream_t st) {
     auto kern = mx4_linear_a16_kernel<BF16, MT, NT, NW, 2>;
     constexpr size_t lds = (size_t)NW * MT * NT * 4 * 64 * sizeof(float);
     a.tiles_n = (int)(((long)a.N + 16 * NT - 1) / (16 * NT));
-    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));
-    if (!grid_fits(tiles, NW * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const long tiles = (long)a.tiles_n * (((long)a.M + 16 * MT - 1) / (16 * MT));     // (mx4_way has asked whether they are a launch)
     static KernelState ks;
     if (prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks) < 0) return W4A4_ERR_HIP;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(NW * 64), lds, st, a);
@@ -162,16 +161,18 @@ int launch(A16Args a, hipStream_t st) {
 // Tokens and channels of a tile, waves that share K.  Fitted to 200 sizes of 1 to 64 tokens each; over 200 with weights that no cache holds the choice is 2.2 % above the
 // best of nine kinds, 32 % at worst.  us of the kinds in their order: one token 4096 x 4096 5.5, 4.8, ..; 32 tokens 16000 x 4096 (23 by the third), 20, 19, 32, 17; 64 tokens
 // 32000 x 768 (28), 17, 22, 16, 22.
-constexpr MX4Way kWays[] = {{16, 16, 0, 2.405f, 0.114f, 0.099f, 0.224f, 0.0f}, {16, 16, 0, 2.596f, 0.087f, 0.103f, 0.448f, 0.0f}, {16, 32, 0, 2.743f, 0.129f, 0.143f, 0.756f, 0.0f},
-                            {16, 64, 0, 3.126f, 0.273f, 0.218f, 0.531f, 0.0f}, {16, 64, 0, 3.301f, 0.206f, 0.229f, 1.126f, 0.0f}, {32, 64, 0, 3.390f, 0.808f, 0.293f, 1.070f, 0.0f},
-                            {32, 64, 0, 3.698f, 0.296f, 1.413f, 0.000f, 0.0f}};
+constexpr MX4Way kWays[] = {{16, 16, 256, 0, 2.405f, 0.114f, 0.099f, 0.224f, 0.0f}, {16, 16, 512, 0, 2.596f, 0.087f, 0.103f, 0.448f, 0.0f}, {16, 32, 512, 0, 2.743f, 0.129f, 0.143f, 0.756f, 0.0f},
+                            {16, 64, 256, 0, 3.126f, 0.273f, 0.218f, 0.531f, 0.0f}, {16, 64, 512, 0, 3.301f, 0.206f, 0.229f, 1.126f, 0.0f}, {32, 64, 128, 0, 3.390f, 0.808f, 0.293f, 1.070f, 0.0f},
+                            {32, 64, 512, 0, 3.698f, 0.296f, 1.413f, 0.000f, 0.0f}};
 
 template <bool BF16>
 int pick(const A16Args &a, hipStream_t st) {
+    constexpr int ways = (int)(sizeof(kWays) / sizeof(kWays[0]));
+    if (!mx4_any_launches(kWays, ways, a.M, a.N)) return W4A4_ERR_UNSUPPORTED_SHAPE;
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(mx4_linear_a16_kernel<BF16, 1, 1, 8, 2>), 0, ks);
     if (cus < 0) return W4A4_ERR_HIP;
-    switch (mx4_way(kWays, (int)(sizeof(kWays) / sizeof(kWays[0])), a.M, a.N, mx4_planes(a.K), a.act, cus)) {
+    switch (mx4_way(kWays, ways, a.M, a.N, mx4_planes(a.K), a.act, cus)) {
         case 0: return launch<BF16, 1, 1, 4>(a, st);
         case 1: return launch<BF16, 1, 1, 8>(a, st);
         case 2: return launch<BF16, 1, 2, 8>(a, st);
@@ -193,7 +194,6 @@ extern "C" int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, con
     if (M == 0) return W4A4_OK;
     if (!X || !out) return W4A4_ERR_INVALID_ARG;
     if (W->rows % 8 || ldx % 8 || ldx >= 1 << 24 || !aligned16(X) || !aligned16(out) || (bias && !aligned16(bias))) return W4A4_ERR_UNSUPPORTED_SHAPE;
-    if (((long)M / 16 + 1) * ((long)W->rows / 16 + 1) > 0x7fffffffL) return W4A4_ERR_UNSUPPORTED_SHAPE;          // (of the smallest tiles: a grid)
     const A16Args a{static_cast<const uint16_t *>(X), W->q, W->scale, static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(out), M, W->rows, W->K, ldx, act, 0};
     return dtype == W4A4_BF16 ? pick<true>(a, as_stream(stream)) : pick<false>(a, as_stream(stream));
 }

@@ -266,15 +266,14 @@ int launch(MX4LinearArgs g, hipStream_t st) {
     static_assert(lds <= 160 * 1024, "a CU's LDS");
     g.tiles_m = (int)(((long)g.M + BM - 1) / BM);
     g.tiles_n = (int)(((long)g.N + BN - 1) / BN);
-    const long tiles = (long)g.tiles_m * g.tiles_n;
-    if (!grid_fits(tiles, WM * WN * KS * 64)) return W4A4_ERR_UNSUPPORTED_SHAPE;
+    const long tiles = (long)g.tiles_m * g.tiles_n;                // (mx4_way has asked whether they are a launch)
     static KernelState ks;
     const int cus = prepare_kernel(reinterpret_cast<const void *>(kern), lds, ks);
     if (cus < 0) return W4A4_ERR_HIP;
     g.whole = (int)tiles;
     if (TAIL) {
         const int slots = cus, left = (int)(tiles % slots);
-        if (tiles > slots && 4 * left <= slots) g.whole = (int)tiles - left;
+        if (tiles > slots && 4 * left <= slots && grid_fits(tiles + 3 * left, WM * WN * KS * 64)) g.whole = (int)tiles - left;
     }
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.whole + 4 * (tiles - g.whole))), dim3(WM * WN * KS * 64), lds, st, g);
     return launch_status();

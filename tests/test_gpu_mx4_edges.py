@@ -1,4 +1,4 @@
-"""Products of microscaled 4-bit floating point where their results are easy to get wrong: GELU of every bf16 number."""
+"""Products of microscaled 4-bit floating point where their results are easy to get wrong: GELU of every bf16 number, dimensions that pass a launch of some kinds of tiles."""
 import pytest
 import torch
 
@@ -38,3 +38,29 @@ def test_gelu_of_every_bf16_number(B, M, a16):
     # half a step is 2^-8 of the value at worst and 2^-9 at best: as close counted in steps
     step = torch.exp2(torch.floor(torch.log2(want.abs().clamp(min=2.0 ** -126))) - 7)
     assert (off <= 7.5e-5 * want.abs() + step / 2 * (1 + 2.0 ** -8) + 2.0 ** -122).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,N", [(1, 2 ** 27), (2 ** 27, 8), (2 ** 27 + 3, 16)])
+def test_products_of_a_dimension_that_some_kinds_of_tiles_do_not_launch(B, M, N, dtype):
+    """2^27 rows are 2^23 tiles of 16, 2^32 threads of them: another kind takes such a call.  Zeros but for some rows, of whole numbers whose sums are exact."""
+    g = torch.Generator().manual_seed(3)
+    rows, few, K = max(M, N), min(M, N), 32
+    tall, flat = B.MX4.new(rows, K), B.mx4_quantize(torch.randint(-4, 5, (few, K), generator=g).bfloat16().cuda())
+    tall.q.zero_()
+    tall.scale.fill_(0x7F)
+    at = torch.tensor([0, 15, 16, 255, 257, rows // 2, rows - 33, rows - 17, rows - 1])
+    x = torch.randint(-4, 5, (len(at), K), generator=g).bfloat16().cuda()
+    some = B.mx4_quantize(x)
+    tall.q[:, at.cuda()], tall.scale[:, at.cuda()] = some.q, some.scale
+    values, others = (B.mx4_dequantize(t).cpu().double() for t in (some, flat))
+    if M == rows:
+        got = B.mx4_linear(tall, flat, dtype=dtype)
+        assert torch.equal(got[at.cuda()].cpu().double(), (values @ others.t()).to(dtype).double())
+        got[at.cuda()] = 0
+    else:
+        for got in (B.mx4_linear(flat, tall, dtype=dtype), B.mx4_linear_a16(B.mx4_dequantize(flat, dtype), tall)):
+            assert torch.equal(got[:, at.cuda()].cpu().double(), (others @ values.t()).to(dtype).double())
+            got[:, at.cuda()] = 0
+            assert not got.any()
+    assert not got.any()
