@@ -606,8 +606,8 @@ typedef struct {
 } w4a4_rotary_angles;
 
 /* out[t, h, :] = X[t, h, :] turned by positions[t]; X and out in `dtype`, rows of heads * features numbers ldx and ldo elements apart (multiples of 8);
- * out may be X (ldo == ldx), else the two do not overlap.  Rows of a negative position are copied.  Angles and products are fp32 (2^-22 of a pair's
- * length in all), the result is rounded once.  features: a multiple of 8, 256 at most.  Fastest where pairs is a multiple of 8 or pairs are neighbours. */
+ * out may be X (ldo == ldx), else the two do not overlap.  Rows of a negative position are copied.  Angles and products are fp32 (2^-21.6 of a pair's
+ * length at most in all, 2^-22.6 measured), the result is rounded once.  features: a multiple of 8, 256 at most.  Fastest where pairs is a multiple of 8 or pairs are neighbours. */
 int w4a4_rotary(const void *X, int dtype, int tokens, int heads, int features, int ldx, const int32_t *positions,
                 const w4a4_rotary_angles *R, void *out, int ldo, void *stream);
 
