@@ -5,8 +5,8 @@ Its layers are the encoder's (post-LayerNorm, GELU feed-forward) with causal att
     x  = LN1(x + attn_out(attention(qkv(x))))        qkv, attn_out, ffn1, ffn2: w4a4_linear_w4a16 (4-bit weights, fp16 activations)
     x  = LN2(x + ffn2(gelu(ffn1(x))))                attention: w4a4_kv8_append, w4a4_kv8_attention
 
-Weights may be in microscaled 4-bit floating point instead (weights="mx4"): few tokens go through w4a4_mx4_linear_a16, more of them, prompts above all, are
-quantized and go through w4a4_mx4_linear.  Positions come from a table of embeddings, or queries and keys are turned by them (angles: w4a4_kv8_append_rotary).
+Weights may be in microscaled 4-bit floating point instead (weights="mx4"): single tokens and logits go through w4a4_mx4_linear_a16, the activations of prompts are
+quantized too and go through w4a4_mx4_linear (`activations`: when, if at all).  Positions come from a table of embeddings, or queries and keys are turned by them (angles: w4a4_kv8_append_rotary).
 
 A step takes any number of new tokens of each request (a prompt, a few, one, none, or the end of a request); w4a4_kv8_plan keeps the books of
 blocks on the device.  All layers share one block table.  `python -m paper_2301_12017_amd.decoder` runs random weights.
@@ -38,9 +38,13 @@ class Books:
         return call
 
 
-# Tokens up to which microscaled weights meet activations as they are: the weights are read again for every 64 of them.  us of the product with 16-bit
-# activations | of quantizer and product, 4096 x 4096: 16 tokens 5.4 | 6.0, 64 10.0 | 7.0 (where quantizing costs accuracy and saves little).
+# Tokens of a step up to which microscaled weights meet activations as they are, whatever they are: the weights are read again for every 16 or 32 of them.  us of the product
+# with 16-bit activations | of quantizer and product: 4096 x 4096 16 tokens 5.2 | 6.8, 64 9.3 | 7.0, 128 12.8 | 9.1, 512 42 | 14; 32000 x 768 64 tokens 13 | 7, 512 82 | 15.
 FEW = 64
+
+# When more of them are quantized: where a request has several new tokens ("prompts"), so that a request's single tokens do not depend on how many others there are; never ("16 bits");
+# always ("4 bits").  Quantizing a row moves its numbers by up to a quarter of them, or of its block's power of two.  Rows of logits are never quantized.
+ACTIVATIONS = ("prompts", "16 bits", "4 bits")
 
 
 def quantized(W: torch.Tensor, weights="int4", mode=B.SYM, group=128):
@@ -50,22 +54,24 @@ def quantized(W: torch.Tensor, weights="int4", mode=B.SYM, group=128):
     return B.quantize_weight(W, mode, group) if weights == "int4" else B.mx4_quantize(W)
 
 
-def linear(x: torch.Tensor, W, bias=None, act=B.ACT_NONE) -> torch.Tensor:
-    """x [tokens, K] (fp16) times what `quantized` made."""
+def linear(x: torch.Tensor, W, bias=None, act=B.ACT_NONE, exact=True) -> torch.Tensor:
+    """x [tokens, K] (fp16) times what `quantized` made.  exact: x as it is; else more than FEW rows are quantized where the weights are microscaled."""
     if isinstance(W, B.QWeight):
         return B.linear_w4a16(x, W, bias, act)
-    if len(x) <= FEW:
+    if exact or len(x) <= FEW:
         return B.mx4_linear_a16(x, W, bias, act)
     return B.mx4_linear(B.mx4_quantize(x), W, bias, act, x.dtype)
 
 
 class DecoderLayer:
     """One layer: 4-bit weights (see `quantized`), a cache of `blocks` blocks.  heads: of queries; kv_heads: of keys and values (grouped heads).  angles: what
-    queries and keys are turned by (RotaryAngles), None where positions are in the embeddings."""
+    queries and keys are turned by (RotaryAngles), None where positions are in the embeddings.  activations: one of ACTIVATIONS, of microscaled weights."""
 
     def __init__(self, Wqkv, bqkv, Wo, bo, W1, b1, W2, b2, g1, be1, g2, be2, heads: int, kv_heads: int, blocks: int, block=16, group=128, mode=B.SYM, eps=1e-12,
-                 weights="int4", angles=None):
-        hidden = Wo.shape[0]
+                 weights="int4", angles=None, activations="prompts"):
+        if activations not in ACTIVATIONS:
+            raise ValueError(f"activations {activations!r}: one of {ACTIVATIONS}")
+        hidden, self.activations = Wo.shape[0], activations
         self.heads, self.kv_heads, self.features, self.eps = heads, kv_heads, Wo.shape[1] // heads, eps
         assert Wqkv.shape == ((heads + 2 * kv_heads) * self.features, hidden)
         self.qkv, self.out, self.ffn1, self.ffn2 = (quantized(W, weights, mode, group) for W in (Wqkv, Wo, W1, W2))
@@ -75,15 +81,16 @@ class DecoderLayer:
 
     def __call__(self, x: torch.Tensor, books: Books, plan: B.PreparedKV8Plan, queries: int) -> torch.Tensor:
         T, D = x.shape[0], self.features
-        q, k, v = (t.view(T, -1, D) for t in linear(x, self.qkv, self.bias[0]).split([self.heads * D, self.kv_heads * D, self.kv_heads * D], 1))
+        exact = self.activations == "16 bits" or self.activations == "prompts" and queries <= 1
+        q, k, v = (t.view(T, -1, D) for t in linear(x, self.qkv, self.bias[0], exact=exact).split([self.heads * D, self.kv_heads * D, self.kv_heads * D], 1))
         if self.angles is None:
             B.kv8_append(self.cache, k, v, plan.slots)
         else:
             q = B.kv8_append_rotary(self.cache, k, v, plan.slots, plan.positions, self.angles, q)
         a = B.kv8_attention(q, self.cache, books.table, plan.lens, plan.start, queries, books.context, D ** -0.5, workspace=books.workspace)
-        x = self._norm(linear(a.view(T, -1), self.out, self.bias[1]), x, self.ln1)
-        h = linear(x, self.ffn1, self.bias[2], B.ACT_GELU)
-        return self._norm(linear(h, self.ffn2, self.bias[3]), x, self.ln2)
+        x = self._norm(linear(a.view(T, -1), self.out, self.bias[1], exact=exact), x, self.ln1)
+        h = linear(x, self.ffn1, self.bias[2], B.ACT_GELU, exact)
+        return self._norm(linear(h, self.ffn2, self.bias[3], exact=exact), x, self.ln2)
 
     def _norm(self, x, residual, ln):
         return B.layernorm_quantize(x, residual, ln[0], ln[1], self.eps)[1]
@@ -142,7 +149,7 @@ class Decoder:
 
 
 def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabulary=1000, requests=4, context=512, block=16, group=128, mode=B.SYM, seed=0,
-                   weights="int4", rotary=False) -> Decoder:
+                   weights="int4", rotary=False, activations="prompts") -> Decoder:
     """Random weights of the given sizes, and blocks for `requests` requests of `context` tokens.  rotary: no position embeddings, queries and keys turn."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     normal = lambda *shape, std=0.02: (torch.randn(shape, generator=g, device="cuda") * std).half()
@@ -152,7 +159,8 @@ def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabul
     one = lambda: (1 + normal(hidden, std=0.05).float()).half()
     made = [DecoderLayer(normal((heads + 2 * kv_heads) * D, hidden, std=0.05), normal((heads + 2 * kv_heads) * D), normal(hidden, heads * D), normal(hidden),
                          normal(ffn, hidden), normal(ffn), normal(hidden, ffn), normal(hidden), one(), normal(hidden), one(), normal(hidden),
-                         heads, kv_heads, blocks, block, group, mode, weights=weights, angles=angles) for _ in range(layers)]
+                         heads, kv_heads, blocks, block, group, mode, weights=weights, angles=angles,
+                         activations=activations) for _ in range(layers)]
     return Decoder(made, normal(vocabulary, hidden, std=1.0), None if rotary else normal(books.context, hidden, std=0.3), books, group, weights)
 
 
