@@ -47,11 +47,16 @@ FEW = 64
 ACTIVATIONS = ("prompts", "16 bits", "4 bits")
 
 
-def quantized(W: torch.Tensor, weights="int4", mode=B.SYM, group=128):
-    """W [N, K] (fp16) in the 4-bit form asked for: integer codes in groups ("int4") or microscaled floating point ("mx4")."""
+def quantized(W: torch.Tensor, weights="int4", mode=None, group=None):
+    """W [N, K] (fp16) in the 4-bit form asked for: integer codes ("int4", symmetric ones in groups of 128 where nothing else is said) or microscaled floating
+    point ("mx4", which has neither modes nor groups)."""
     if weights not in ("int4", "mx4"):
         raise ValueError(f"weights {weights!r}: int4 or mx4")
-    return B.quantize_weight(W, mode, group) if weights == "int4" else B.mx4_quantize(W)
+    if weights == "int4":
+        return B.quantize_weight(W, B.SYM if mode is None else mode, 128 if group is None else group)
+    if mode is not None or group is not None:
+        raise ValueError(f"mode {mode}, group {group}: microscaled weights have blocks of 32 and no mode")
+    return B.mx4_quantize(W)
 
 
 def linear(x: torch.Tensor, W, bias=None, act=B.ACT_NONE, exact=True) -> torch.Tensor:
@@ -67,7 +72,7 @@ class DecoderLayer:
     """One layer: 4-bit weights (see `quantized`), a cache of `blocks` blocks.  heads: of queries; kv_heads: of keys and values (grouped heads).  angles: what
     queries and keys are turned by (RotaryAngles), None where positions are in the embeddings.  activations: one of ACTIVATIONS, of microscaled weights."""
 
-    def __init__(self, Wqkv, bqkv, Wo, bo, W1, b1, W2, b2, g1, be1, g2, be2, heads: int, kv_heads: int, blocks: int, block=16, group=128, mode=B.SYM, eps=1e-12,
+    def __init__(self, Wqkv, bqkv, Wo, bo, W1, b1, W2, b2, g1, be1, g2, be2, heads: int, kv_heads: int, blocks: int, block=16, group=None, mode=None, eps=1e-12,
                  weights="int4", angles=None, activations="prompts"):
         if activations not in ACTIVATIONS:
             raise ValueError(f"activations {activations!r}: one of {ACTIVATIONS}")
@@ -100,14 +105,14 @@ class Decoder:
     """Token and position embeddings (positions None: the layers turn queries and keys), layers, and the logits of the tokens' successors from the
     quantized token embeddings."""
 
-    def __init__(self, layers, tokens: torch.Tensor, positions, books: Books, group=128, weights="int4"):
+    def __init__(self, layers, tokens: torch.Tensor, positions, books: Books, group=None, weights="int4"):
         if positions is None and not all(layer.angles for layer in layers):
             raise ValueError("no position embeddings, and layers without angles")
         if positions is not None and len(positions) < books.context:       # (the plan hands out every position of a block, and they are looked up unseen)
             raise ValueError(f"{len(positions)} position embeddings for requests of up to {books.context} tokens")
         self.layers, self.tokens, self.positions, self.books = layers, tokens, positions, books
         pad = -len(tokens) % 8                             # (the linear's channels come in eights)
-        self.head = quantized(torch.nn.functional.pad(tokens, (0, 0, 0, pad)).contiguous(), weights, B.SYM, group)
+        self.head = quantized(torch.nn.functional.pad(tokens, (0, 0, 0, pad)).contiguous(), weights, None, group)
 
     def step(self, ids: torch.Tensor, new_tokens: torch.Tensor, queries: int):
         """ids [tokens]: the new tokens of all requests, one after the other, new_tokens [requests] of them each and `queries` at most.  Returns the
@@ -148,7 +153,7 @@ class Decoder:
         return torch.stack(found, 1)
 
 
-def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabulary=1000, requests=4, context=512, block=16, group=128, mode=B.SYM, seed=0,
+def random_decoder(layers=2, hidden=768, heads=12, kv_heads=4, ffn=2048, vocabulary=1000, requests=4, context=512, block=16, group=None, mode=None, seed=0,
                    weights="int4", rotary=False, activations="prompts") -> Decoder:
     """Random weights of the given sizes, and blocks for `requests` requests of `context` tokens.  rotary: no position embeddings, queries and keys turn."""
     g = torch.Generator(device="cuda").manual_seed(seed)
