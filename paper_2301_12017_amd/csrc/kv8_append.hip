@@ -461,9 +461,11 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
     else write(std::false_type{});
 }
 
-// (Turning keys takes some 165 registers: three waves a SIMD.)
+// Waves a SIMD: turning keys takes up to 168 registers, three of them.  Heads of 256 keep 11 to 13 of theirs in scratch memory for that, which is still the faster way (us by
+// three | two waves, two heads: 3000 tokens in blocks of 32 12 | 16, 12003 in blocks of 16 22.5 | 23.6, 4000 in blocks of 64 22.8 | 21.6), and all keep 90 to 125 scalar ones in
+// lanes of a vector register.  Without positions heads of 96 need 93 where they are told to, and five waves run; by themselves they take 97.
 template <bool BF16, int D, Positions POSITIONS>
-__global__ __launch_bounds__(256, POSITIONS == kNone ? 1 : 3) void kv8_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256, POSITIONS != kNone ? 3 : D == 96 ? 5 : 1) void kv8_append_kernel(AppendArgs a) {
     constexpr bool ROTARY = POSITIONS != kNone;
     extern __shared__ __attribute__((aligned(16))) float angles[]; // ROTARY: a window's
     __shared__ uint32_t ranges[8];
