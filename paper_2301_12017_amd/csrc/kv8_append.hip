@@ -35,6 +35,9 @@ struct AppendArgs {
     long ld[2];
     const int32_t *slots;
     int T, blocks, H, shift, tile;
+};
+// (The append without positions is a call of few microseconds, and takes 0.1 of them less without these 144 bytes of arguments, of which it reads none: 200 single tokens 4.48 -> 4.37.)
+struct TurningArgs : AppendArgs {
     int waves, window, query_tile;                                 // that share a run; tokens whose angles are there at once; tokens whose queries a workgroup turns
     const int32_t *positions;                                      // keys that turn
     RotaryArgs r;
@@ -181,7 +184,7 @@ struct Window {
     int *positions;
     uint64_t turns[2];                                             // of the lane's pairs
     int first, count;
-    __device__ __forceinline__ void open(const AppendArgs &a, float *lds) {
+    __device__ __forceinline__ void open(const TurningArgs &a, float *lds) {
         const int lane = threadIdx.x & 63, last = a.r.pairs - 1;
         cosines = lds;
         sines = lds + a.window * a.r.pairs;
@@ -190,7 +193,7 @@ struct Window {
         turns[0] = a.r.turns[min(lane, last)];
         turns[1] = a.r.turns[min(lane + 64, last)];
     }
-    __device__ __forceinline__ void fill(const AppendArgs &a, int from, int tokens) {
+    __device__ __forceinline__ void fill(const TurningArgs &a, int from, int tokens) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pairs = a.r.pairs;
         if (count) __syncthreads();                                // (the angles before have been read)
         first = from;
@@ -266,7 +269,7 @@ struct Turning {
 
 // Keys with positions: tokens t0 .. t1-1 into the block's rows (h past the last head: nothing, but in step).
 template <bool BF16, int D>
-__device__ __forceinline__ void append_turned_keys(const AppendArgs &a, int t0, int t1, int b, int h, bool first, int lane, Window &window, const Share &share) {
+__device__ __forceinline__ void append_turned_keys(const TurningArgs &a, int t0, int t1, int b, int h, bool first, int lane, Window &window, const Share &share) {
     constexpr int LANES = Turning<D>::LANES, ROWS = Turning<D>::ROWS, N = Turning<D>::N, CHUNK = Turning<D>::CHUNK;
     const int block = 1 << a.shift, row = min(lane / LANES, ROWS - 1), d = lane % LANES * 8, pairs = a.r.pairs, step = share.waves * CHUNK;
     const bool there = h < a.H, on = lane / LANES < ROWS && there;
@@ -465,7 +468,7 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, int t0, int t
 // three | two waves, two heads: 3000 tokens in blocks of 32 12 | 16, 12003 in blocks of 16 22.5 | 23.6, 4000 in blocks of 64 22.8 | 21.6), and all keep 90 to 125 scalar ones in
 // lanes of a vector register.  Without positions heads of 96 need 93 where they are told to, and five waves run; by themselves they take 97.
 template <bool BF16, int D, Positions POSITIONS>
-__global__ __launch_bounds__(256, POSITIONS != kNone ? 3 : D == 96 ? 5 : 1) void kv8_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256, POSITIONS != kNone ? 3 : D == 96 ? 5 : 1) void kv8_append_kernel(std::conditional_t<POSITIONS == kNone, AppendArgs, TurningArgs> a) {
     constexpr bool ROTARY = POSITIONS != kNone;
     extern __shared__ __attribute__((aligned(16))) float angles[]; // ROTARY: a window's
     __shared__ uint32_t ranges[8];
@@ -501,7 +504,8 @@ __global__ __launch_bounds__(256, POSITIONS != kNone ? 3 : D == 96 ? 5 : 1) void
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> a.shift) < a.blocks ? slot >> a.shift : -1; };   // -1: not stored
     // slots of the token before the tile and of the 63 from its first one on; where runs begin; where a slot does not follow the one before
     const int at = t_first - 1 + lane, read = a.slots[min(max(at, 0), a.T - 1)];
-    if (ROTARY && !values && a.tile == 1) window.fill(a, t_first, 1);                   // (while the slots are on their way)
+    if constexpr (ROTARY)
+        if (!values && a.tile == 1) window.fill(a, t_first, 1);    // (while the slots are on their way)
     const int slot = at >= 0 && at < a.T ? read : -1, b = block_of(slot);
     const int b_before = __shfl_up(b, 1, 64), slot_before = __shfl_up(slot, 1, 64);
     const unsigned long long begins = __ballot(lane > 0 && b != b_before), jumps = __ballot(lane > 0 && slot != slot_before + 1);
@@ -692,14 +696,18 @@ int rows_check(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype,
 template <Positions POSITIONS>
 int append(const w4a4_kv8_cache *C, const void *K, const void *V, int dtype, int tokens, int ldk, int ldv, const int32_t *slots, const int32_t *positions,
            const RotaryArgs &r, const RotaryWork &q, hipStream_t st) {
-    AppendArgs a{C->k, C->v, C->k_scale, C->v_scale, {static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V)}, {ldk, ldv},
-                 slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece, 1, 0, 1, positions, r, q};
+    std::conditional_t<POSITIONS == kNone, AppendArgs, TurningArgs> a;
+    static_cast<AppendArgs &>(a) = {C->k, C->v, C->k_scale, C->v_scale, {static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V)}, {ldk, ldv},
+                                    slots, tokens, C->blocks, C->heads, __builtin_ctz(C->block), tokens <= 512 ? 1 : kPiece};
     return by_features(C->features, [&](auto d) {
         constexpr int D = decltype(d)::value, CHUNK = Turning<D>::CHUNK, WAVES = Turning<D>::WAVES;
         static_assert(WAVES * CHUNK <= 64, "a lane each");
         size_t lds = 0;
         dim3 grid((tokens + a.tile - 1) / a.tile, (2 * C->heads + 3) / 4);
-        if (POSITIONS != kNone) {
+        if constexpr (POSITIONS != kNone) {
+            a.positions = positions;
+            a.r = r;
+            a.q = q;
             const int share = C->block / (D == 256 ? 8 : 16);
             a.waves = share < WAVES ? share : WAVES;
             // (a workgroup for a token each: sharing leaves few of its waves something to do, so not where there are many; 200 tokens of 8 heads of 64 13 us shared, 8 not)

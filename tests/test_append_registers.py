@@ -73,3 +73,10 @@ def test_waves_of_the_append_with_positions(appends, D, positions):
     assert len(kernels) == 2
     for k in kernels:
         assert k[".vgpr_count"] <= 168 and k[".vgpr_spill_count"] <= (13 if D == 256 else 0), k
+
+
+def test_arguments_of_the_append_without_positions(appends):
+    """What the host copies for each call: nothing of positions, angles and queries."""
+    for D in (64, 96, 128, 256):
+        for k in _of(appends, D, 0):
+            assert sum(a[".size"] for a in k[".args"] if a[".value_kind"] == "by_value") == 96
