@@ -680,7 +680,7 @@ int w4a4_mx4_dequantize(const w4a4_mx4 *Q, int dtype, void *X, void *stream);
 int w4a4_mx4_linear(const w4a4_mx4 *A, const w4a4_mx4 *W, const void *bias, int act, int dtype, void *out, void *stream);
 
 /* The same with activations X [M, ldx] (first W->K columns) in `dtype`, not quantized: for up to 64 tokens, where the bytes of W are the cost (W is read again for
- * every 64).  A block's 32 products are summed before its power of two comes to them: an |x| past 2^120 may pass fp32 there.  ldx a multiple of 8, below 2^24;
+ * every 16 or 32).  A block's 32 products are summed before its power of two comes to them: an |x| past 2^120 may pass fp32 there.  ldx a multiple of 8, below 2^24;
  * ceil(M / 32) * ceil(N / 64) below 2^25. */
 int w4a4_mx4_linear_a16(const void *X, int dtype, int M, int ldx, const w4a4_mx4 *W, const void *bias, int act, void *out, void *stream);
 

@@ -1047,7 +1047,8 @@ def rotary_frequencies(pairs: int, base=10000.0, factor=1.0, trained=0, slow=1.0
 
 class RotaryAngles:
     """What w4a4_rotary turns by (w4a4_rotary_angles in include/w4a4.h): frequencies in radians a position, one for each pair (64 bits keep far positions
-    exact), pairs of neighbours or of halves, and what cosines and sines are multiplied by."""
+    exact), pairs of neighbours or of halves, and what cosines and sines are multiplied by.  Made once for a model: exact fractions take some 8 us a pair on the host,
+    and frequencies that lie on a device are waited for."""
 
     def __init__(self, frequencies, interleaved=False, magnitude=1.0, device="cuda"):
         f = torch.as_tensor(frequencies, dtype=torch.float64).cpu()

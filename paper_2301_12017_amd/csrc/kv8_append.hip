@@ -9,15 +9,15 @@
 // two neighbouring features (one where D is 64) of sixteen tokens and writes each feature's codes as one sixteen-byte
 // piece of the block.  A run of at most sixteen tokens is read once, a longer one a second time out of L2.
 //
-// Long runs: 12005 tokens of 8 heads of 128 features in blocks of 16, fp16, 28.6 us = 2.6 TB/s of 74 MB.  A wave takes its runs one after the
+// Long runs: 12005 tokens of 8 heads of 128 features in blocks of 16, fp16, 25 us = 2.9 TB/s of 74 MB (22 where the rows are in a cache).  A wave takes its runs one after the
 // other, and in each the rows, their range, the scale and the codes are steps in series, of the keys with a load of the slot in front of
-// each store; other waves fill in.  Reading them back 18.0 us = 4.1 TB/s.  Single tokens are latency, slots to scale to codes: 48 of 8 heads 4.5 us where
+// each store; other waves fill in.  Reading them back 20.8 us = 3.5 TB/s (16).  Single tokens are latency, slots to scale to codes: 48 of 8 heads 4.5 us where
 // most scales stay, 6.0 where all of them rise and their blocks are re-scaled (the long runs, of which few meet older codes: 2.1 more); 4.6 to read 832.
 //
 // With positions, keys are turned (rotary.hpp) on their way in, in fp32: what is stored is the turned key rounded once, to its code.  Workgroups of four waves take
 // one, two or four heads, waves that have the same head share its runs, and all four find the angles of a step together, in LDS.  Queries are workgroups of the same launch.
-// 48 single tokens of 8 heads of 128, 32 heads of queries: 6.6 us, slots beside positions to angles to range to codes in a chain.  12003 tokens of prompts in blocks of 16 35 us
-// (without positions 24), with 32 heads of queries 70 to 76 = 3.6 TB/s: the steps of a run in series, where turning takes registers (three waves a SIMD, vector ALU 37 % busy).
+// 48 single tokens of 8 heads of 128, 32 heads of queries: 6.6 us, slots beside positions to angles to range to codes in a chain.  12003 tokens of prompts in blocks of 16 36 us
+// (without positions 25), with 32 heads of queries 70 to 76 = 3.6 TB/s: the steps of a run in series, where turning takes registers (three waves a SIMD, vector ALU 37 % busy).
 #include "rotary.hpp"
 
 namespace w4a4 {

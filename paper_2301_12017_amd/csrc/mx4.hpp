@@ -59,7 +59,7 @@ __device__ __forceinline__ uint16_t mx4_result(float y, bool gelu) {
 }
 
 // Tiles of a product.  A problem of M x N and `planes` of K takes about  start + plane * planes + (more * planes + tile) * (tiles / CUs - 1, not below 0)  us
-// by tiles of one kind: small ones bring the operands of a small problem to more CUs (a CU takes in some 65 GB/s, whatever is asked for at once), large ones
+// by tiles of one kind: small ones bring the operands of a small problem to more CUs (42 to 52 KB a us come into a CU by the constants, whatever is asked for at once), large ones
 // bring less in all.  Past the `held` tiles of a CU the count lies halfway between tiles and whole rounds of them.
 // A kind whose workgroups are more than a launch takes is none.
 struct MX4Way {

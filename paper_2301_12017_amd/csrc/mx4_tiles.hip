@@ -12,8 +12,8 @@
 //
 // What bounds it: 8192 x 8192 x 8192 263 us = 4.2 PFLOP/s by tiles of 256 x 256, of 6.1 that registers full of such operands reach (8.9 where they are zeros: it is the
 // power that is short); without its DMA 214, without its stores 247, on zeros 204; matrix pipe 58 % of the cycles, no conflict in LDS.  Small K is bound by the
-// results: 16384 x 16384 x 1024 195 us = 2.8 TB/s of results by 128 x 256, and 229 with GELU, whose eleven instructions a number are 50 us of every SIMD's time and
-// run beside other workgroups' products only in part.  Few tokens are bound by what a CU takes in: 301 tokens 4096 x 1056 5.0 us by 64 x 128.
+// results: 16384 x 16384 x 1024 195 us = 2.8 TB/s of results by 128 x 256, and 229 with fp16's GELU, whose eleven instructions a number are 50 us of every SIMD's time and
+// (bf16's has fifteen: 13 us more) run beside other workgroups' products only in part.  Few tokens are bound by what a CU takes in: 301 tokens 4096 x 1056 5.0 us by 64 x 128.
 #include "gemm_common.hpp"
 #include "mx4.hpp"
 #include "mx4_linear.hpp"
