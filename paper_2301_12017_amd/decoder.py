@@ -42,8 +42,8 @@ class Books:
 # with 16-bit activations | of quantizer and product: 4096 x 4096 16 tokens 5.2 | 6.8, 64 9.3 | 7.0, 128 12.8 | 9.1, 512 42 | 14; 32000 x 768 64 tokens 13 | 7, 512 82 | 15.
 FEW = 64
 
-# When more of them are quantized: where a request has several new tokens ("prompts"), so that a request's single tokens do not depend on how many others there are; never ("16 bits");
-# always ("4 bits").  Quantizing a row moves its numbers by up to a quarter of them, or of its block's power of two.  Rows of logits are never quantized.
+# When more of them are quantized: in steps where a request has several new tokens ("prompts"; all rows of such a step are), so that steps of single tokens do not depend on how many
+# requests there are; never ("16 bits"); always ("4 bits").  Quantizing a row moves its numbers by up to a quarter of them, or of its block's power of two.  Rows of logits are never quantized.
 ACTIVATIONS = ("prompts", "16 bits", "4 bits")
 
 
